@@ -261,6 +261,122 @@ lstm_status_t lstm_describe_tiling(lstm_handle_t h, int *out8);
  * both directions' dx). */
 lstm_status_t lstm_add(lstm_dtype_t dtype, size_t n, const void *a, const void *b, void *out, void *stream);
 
+/* --- around the recurrent layers ---------------------------------------------
+ * The operators below join a stack of layers to its tokens and to other
+ * layers: the rows of an embedding, the residual addition with its norm, and
+ * linear attention, a recurrent layer whose state is a matrix per head.  Each
+ * takes sizes and pointers like lstm_add and keeps nothing between calls, so
+ * calls may run at the same time on several streams as long as each has its
+ * own outputs and workspace.  The conventions above hold: device pointers,
+ * activations and weights in `dtype`, gradients of weights in fp32, rows of
+ * activations a stride (in elements) apart, 16-byte alignment, arguments
+ * checked on the host before anything is launched.  No call allocates or
+ * synchronises, and all may be captured into a graph.  Outputs must not share
+ * memory with inputs except where a call says so. */
+
+/* Rows of an embedding picked by tokens and scaled:
+ *   out[n][:] = scale * table[ids[n]][:]     (out row stride ldo; 0 = dense)
+ *   ids [N] (int64, 8-byte aligned), table [V][D] and out [N][D] (dtype); D a multiple of 8.
+ * A token outside 0 .. V-1 (padding) gives a row of zeros.  N = 0 is allowed. */
+lstm_status_t lstm_embed_forward(lstm_dtype_t dtype, long N, long V, int D, const int64_t *ids, const void *table,
+                                 float scale, void *out, long ldo, void *stream);
+
+/* Bytes of `workspace` for lstm_embed_backward. */
+size_t lstm_embed_workspace_size(long N, long V, int D);
+
+/* Gradient of the table:
+ *   dtable[v][:] (+)= scale * sum over n with ids[n] = v of dout[n][:]
+ *   dout [N][D] (dtype, row stride ldo); dtable [V][D] fp32, dense.
+ *   accumulate: 0 overwrites the whole table's gradient (rows that no token
+ *     picks with zeros), 1 adds to it and touches only rows that are picked.
+ * Tokens outside 0 .. V-1 take no part.  Each row is summed in fp32 over its
+ * tokens sorted by position, in an order set by the sizes alone: equal inputs
+ * give equal bits.  N = 0 is allowed.  N and V up to 2^31 - 2^20. */
+lstm_status_t lstm_embed_backward(lstm_dtype_t dtype, long N, long V, int D, const int64_t *ids, const void *dout,
+                                  long ldo, float scale, float *dtable, int accumulate, void *workspace,
+                                  size_t workspace_bytes, void *stream);
+
+/* Residual addition and root-mean-square norm of rows:
+ *   sum = x + res (rounded to `dtype` as lstm_add rounds it)
+ *   y   = sum * g / sqrt(mean of sum^2 over the row + eps)
+ *   x, res, sum, y: [rows][D], dtype, row strides ldx (x), ldr (res and sum)
+ *   and ldy (y), 0 = dense; g [D], dtype; D a multiple of 8, at most 16384.
+ *   res may be NULL: then sum is x, and `sum` may be NULL (if not, it gets x).
+ *   sum may be res, or x when ldx = ldr.  The norm is that of the stored sum.
+ *   The squares are summed in fp32: |sum| up to 1e18.  rows = 0 is allowed. */
+lstm_status_t lstm_add_norm(lstm_dtype_t dtype, long rows, int D, const void *x, long ldx, const void *res, long ldr,
+                            const void *g, float eps, void *sum, void *y, long ldy, void *stream);
+
+/* The same with y in 8 bits, as the operand of an 8-bit product: y8 [rows][D]
+ * (dense, OCP e4m3 bit patterns, round to nearest even) and one fp32 scale per
+ * row, scale = max over the row of |y| / 448, so that y ~ y8 * scale.  A row
+ * whose y is zero throughout has scale 0 and y8 zeros. */
+lstm_status_t lstm_add_norm_q8(lstm_dtype_t dtype, long rows, int D, const void *x, long ldx, const void *res, long ldr,
+                               const void *g, float eps, void *sum, uint8_t *y8, float *scale, void *stream);
+
+/* Bytes of `workspace` for lstm_add_norm_backward. */
+size_t lstm_add_norm_workspace_size(long rows, int D);
+
+/* Gradient of lstm_add_norm for the loss <dy, y> + <dsum, sum>:
+ *   dx (that of x and of res alike), dg [D] fp32, from the forward's stored
+ *   sum (x itself when there was no residual), g and eps.
+ *   dy (row stride ldy); dsum (row stride ldr), the gradient that reaches the
+ *   sum past the norm, NULL means zeros; sum (ldr); dx (ldx).  dx may be dsum
+ *   (ldx = ldr), dy (ldx = ldy) or sum (ldx = ldr).
+ *   accumulate: 0 overwrites dg, 1 adds to it. */
+lstm_status_t lstm_add_norm_backward(lstm_dtype_t dtype, long rows, int D, const void *dy, long ldy, const void *dsum,
+                                     const void *sum, long ldr, const void *g, float eps, void *dx, long ldx, float *dg,
+                                     int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Linear attention with a decay for each head: per batch row and head a state
+ * S of K x M values, and for every step
+ *   S_t = decay S_{t-1} + k_t v_t^T ;   o_t = scale q_t S_t
+ * so that o_t = scale sum_{s <= t} decay^(t-s) (q_t . k_s) v_s plus what is
+ * left of the initial state.  Sequences run in chunks (the sum within a chunk,
+ * the state between chunks), single tokens as the recurrence.
+ *   q, k [T][B][N*K], v, o [T][B][N*M] (head n in columns n*K.. or n*M..), row
+ *   strides ldq, ldk, ldv, ldo between consecutive (t,b) rows: columns of one
+ *   fused projection may be given.  decay [N] fp32, every value in 0 .. 1
+ *   (constants of the layer: they get no gradient).  States [B][N][K][M] fp32. */
+typedef struct {
+    int T, B, N;          /* steps, batch rows, heads */
+    int K, M;             /* key and value width of a head: multiples of 8, 8 .. 256 */
+    lstm_dtype_t dtype;
+    float scale;          /* of the outputs, often 1 / sqrt(K) */
+    long ldq, ldk, ldv, ldo;   /* multiples of 8; 0 = dense */
+} lstm_linattn_desc_t;
+
+/* Bytes of `workspace` for lstm_linattn_forward and lstm_linattn_backward: the
+ * states of the parts a long sequence is split into.  0 for a bad descriptor,
+ * and where nothing is split (the workspace may then be NULL). */
+size_t lstm_linattn_workspace_size(const lstm_linattn_desc_t *d);
+
+/* Outputs of whole sequences.
+ *   lengths [B] int32: steps of each batch row (taken as 0 when negative, as T
+ *     when larger), NULL means T for all.  Rows behind a sequence's end are
+ *     not read; their outputs are zeros.
+ *   S0: initial states, NULL means zeros.  ST: states after each row's last
+ *     step (S0 for a row of length 0), NULL = not wanted; ST may be S0. */
+lstm_status_t lstm_linattn_forward(const lstm_linattn_desc_t *d, const void *q, const void *k, const void *v,
+                                   const float *decay, const int32_t *lengths, const float *S0, void *o, float *ST,
+                                   void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gradients for the loss <do, o> + <dST, ST>, from the forward's inputs.
+ *   do (row stride ldo); dST NULL means zeros.
+ *   dq, dk, dv (row strides ldq, ldk, ldv; zeros behind a sequence's end), dS0:
+ *   NULL = not wanted.  dS0 may be dST. */
+lstm_status_t lstm_linattn_backward(const lstm_linattn_desc_t *d, const void *d_o, const void *q, const void *k,
+                                    const void *v, const float *decay, const int32_t *lengths, const float *S0,
+                                    const float *dST, void *dq, void *dk, void *dv, float *dS0, void *workspace,
+                                    size_t workspace_bytes, void *stream);
+
+/* One token of every batch row (T = 1), for serving: reads S, writes the next
+ * state to S_out (which may be S) and the token's output.  A row whose length
+ * is 0 keeps its state and gets zeros. */
+lstm_status_t lstm_linattn_step(const lstm_linattn_desc_t *d, const void *q, const void *k, const void *v,
+                                const float *decay, const int32_t *lengths, const float *S, float *S_out, void *o,
+                                void *stream);
+
 /* --- kernel timing ----------------------------------------------------------
  * When enabled, every kernel the library launches is bracketed by two HIP
  * events on its own stream, and its algorithmic FLOPs and bytes are recorded

@@ -6,4 +6,4 @@ LSTM / LSTMP layers as hand-written HIP kernels for the MI355X (gfx950).
 use and its absence is an error: there is no fallback path.
 """
 from . import lstm355  # noqa: F401
-from .lstm355 import Layer, Stack, StackLayer, load_library  # noqa: F401
+from .lstm355 import AddNorm, Embedding, Layer, LinearAttention, Stack, StackLayer, load_library  # noqa: F401

@@ -11,6 +11,7 @@
 
 #include "../../include/lstm355.h"
 #include "kernels.hpp"
+#include "status.hpp"
 
 using namespace lstm355;
 
@@ -34,18 +35,15 @@ struct lstm_handle {
 };
 
 namespace {
-
 thread_local char g_detail[256] = "";
-
-void set_detail(const char *what, hipError_t e)
-{
-    std::snprintf(g_detail, sizeof(g_detail), "%s: %s", what, hipGetErrorString(e));
 }
+
+namespace lstm355 {
 
 lstm_status_t hip_status(const char *what, hipError_t e)
 {
     if (e == hipSuccess) return LSTM_OK;
-    set_detail(what, e);
+    std::snprintf(g_detail, sizeof(g_detail), "%s: %s", what, hipGetErrorString(e));
     if (e == hipErrorCooperativeLaunchTooLarge) return LSTM_ERR_UNSUPPORTED;
     return LSTM_ERR_HIP;
 }
@@ -56,16 +54,15 @@ lstm_status_t invalid(const char *what)
     return LSTM_ERR_INVALID_ARG;
 }
 
-size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 lstm_status_t short_buffer(const char *what, size_t given, size_t need)
 {
     std::snprintf(g_detail, sizeof(g_detail), "%s: %zu bytes given, %zu needed", what, given, need);
     return LSTM_ERR_WORKSPACE;
 }
-bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+}  // namespace lstm355
+
+namespace {
 
 lstm_status_t ensure_plan(lstm_handle *h)
 {
@@ -158,12 +155,6 @@ bool forward_xcd(const lstm_handle *h, const RecShape &sh, const void *x, const 
     if (xcd_full_width(sh)) return true;   // these have always needed a y of its own
     return !overlaps_y(h, x, h->TB, h->d.I, h->ldx, y) && !overlaps_y(h, h0, h->d.B, h->Hr, h->Hr, y);
 }
-
-#define TRY_HIP(what, expr)                                  \
-    do {                                                     \
-        hipError_t e_ = (expr);                              \
-        if (e_ != hipSuccess) return hip_status(what, e_);   \
-    } while (0)
 
 }  // namespace
 

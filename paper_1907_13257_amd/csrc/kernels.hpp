@@ -22,6 +22,9 @@ enum KClass {
     K_GEMM_DP,       // dP = dH^T M
     K_SMALL,         // transposes, column sums, fills, adds
     K_GEMM_DWR,      // [dW | dR] = dZ^T [X | H_prev] as one product
+    K_EMBED,         // rows of an embedding, their gradient
+    K_NORM,          // residual norm, forward and backward
+    K_LINATTN,       // linear attention
     K_NCLASS
 };
 const char *kclass_name(int k);

@@ -1,0 +1,301 @@
+// norm.hip -- residual addition and root-mean-square norm of rows, its 8-bit
+// output, and its gradient.
+#include "device_common.hpp"
+#include "operators.hpp"
+
+namespace lstm355 {
+
+namespace {
+
+template <typename T> constexpr int VEC = 16 / (int)sizeof(T);   // elements of a 16-byte access
+
+template <typename T>
+__device__ __forceinline__ void load_vec(const T *p, float (&f)[VEC<T>])
+{
+    T e[VEC<T>];
+    const u32x4 v = ldg16(p);
+    __builtin_memcpy(e, &v, 16);
+#pragma unroll
+    for (int i = 0; i < VEC<T>; ++i) f[i] = to_f32(e[i]);
+}
+
+template <typename T>
+__device__ __forceinline__ void store_vec(T *p, const float (&f)[VEC<T>])
+{
+    T e[VEC<T>];
+#pragma unroll
+    for (int i = 0; i < VEC<T>; ++i) e[i] = from_f32<T>(f[i]);
+    u32x4 v;
+    __builtin_memcpy(&v, e, 16);
+    *reinterpret_cast<u32x4 *>(p) = v;
+}
+
+// 8 (bf16 storage) or 4 (fp32) values as e4m3 bytes, round to nearest even.
+__device__ __forceinline__ unsigned e4m3x4(float a, float b, float c, float d)
+{
+    int v = 0;
+    v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, v, false);
+    v = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
+    return (unsigned)v;
+}
+
+struct Sum2 { float a, b; };
+
+// Sums (a) and sums or maxima (b) over the W waves of a block, in a fixed
+// order; every thread gets both.  `red` holds 2 W floats.
+template <int W, bool MAXB>
+__device__ __forceinline__ Sum2 reduce_row(Sum2 v, float *red)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) {
+        v.a += __shfl_xor(v.a, d);
+        const float o = __shfl_xor(v.b, d);
+        v.b = MAXB ? fmaxf(v.b, o) : v.b + o;
+    }
+    if constexpr (W > 1) {
+        const int wave = threadIdx.x >> 6;
+        __syncthreads();   // the previous row's values have been read
+        if ((threadIdx.x & 63) == 0) {
+            red[2 * wave] = v.a;
+            red[2 * wave + 1] = v.b;
+        }
+        __syncthreads();
+        v = Sum2{red[0], red[1]};
+#pragma unroll
+        for (int w = 1; w < W; ++w) {
+            v.a += red[2 * w];
+            v.b = MAXB ? fmaxf(v.b, red[2 * w + 1]) : v.b + red[2 * w + 1];
+        }
+    }
+    return v;
+}
+
+// A row is held in registers by W waves, P vectors per thread (thread t has
+// vectors t, t + 64 W, ...).  Blocks of W <= 4 waves per row: 4 / W rows at
+// a time in W = 1, one otherwise.
+template <int W> constexpr int ROWS = W == 1 ? 4 : 1;
+template <int W> constexpr int THREADS = W == 1 ? 256 : W * 64;
+
+template <typename T, int W, int P, bool Q8>
+__global__ __launch_bounds__(THREADS<W>) void add_norm_kernel(NormArgs a, int nv)
+{
+    __shared__ float red[2 * W];
+    constexpr int E = VEC<T>;
+    const int tid = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+    for (long row = (long)blockIdx.x * ROWS<W> + (W == 1 ? threadIdx.x >> 6 : 0); row < a.rows;
+         row += (long)gridDim.x * ROWS<W>) {
+        const T *x = static_cast<const T *>(a.x) + row * a.ldx;
+        const T *res = a.res ? static_cast<const T *>(a.res) + row * a.ldr : nullptr;
+        T *sum = a.sum ? static_cast<T *>(a.sum) + row * a.ldr : nullptr;
+        const T *g = static_cast<const T *>(a.g);
+        float s[P][E];
+        Sum2 r{0.0f, 0.0f};
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int c = tid + p * 64 * W;
+            if (c < nv) {
+                load_vec<T>(x + (long)c * E, s[p]);
+                if (res) {
+                    float o[E];
+                    load_vec<T>(res + (long)c * E, o);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) s[p][e] = to_f32(from_f32<T>(s[p][e] + o[e]));
+                }
+                if (sum) store_vec<T>(sum + (long)c * E, s[p]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[p][e] = 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) r.a += s[p][e] * s[p][e];
+            if (c < nv) {
+                float gv[E];
+                load_vec<T>(g + (long)c * E, gv);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    s[p][e] *= gv[e];
+                    if (Q8) r.b = fmaxf(r.b, fabsf(s[p][e]));
+                }
+            }
+        }
+        r = reduce_row<W, true>(r, red);
+        const float rho = rsqrtf(r.a / (float)(nv * E) + a.eps);
+        if constexpr (Q8) {
+            // y / scale = (sum g) 448 / max|sum g|: the norm's factor cancels.
+            // A maximum below the smallest normal number counts as zero.
+            const bool some = !(r.b < 1.17549435e-38f);
+            const float inv = some ? 448.0f / r.b : 0.0f;
+            uint8_t *y = static_cast<uint8_t *>(a.y) + row * (long)nv * E;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int c = tid + p * 64 * W;
+                if (c >= nv) continue;
+                unsigned w[E / 4];
+#pragma unroll
+                for (int q = 0; q < E / 4; ++q)
+                    w[q] = e4m3x4(s[p][4 * q] * inv, s[p][4 * q + 1] * inv, s[p][4 * q + 2] * inv, s[p][4 * q + 3] * inv);
+                __builtin_memcpy(y + (long)c * E, w, E);
+            }
+            if (tid == 0) a.scale[row] = some ? r.b * rho / 448.0f : r.b * 0.0f;
+        } else {
+            T *y = static_cast<T *>(a.y) + row * a.ldy;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int c = tid + p * 64 * W;
+                if (c >= nv) continue;
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[p][e] *= rho;
+                store_vec<T>(y + (long)c * E, s[p]);
+            }
+        }
+    }
+}
+
+// dx = dsum + rho g dy - s rho^3 mean(g dy s); a block adds dy s rho of its
+// rows (a fixed set) in registers and leaves its sums in `partial`.
+template <typename T, int W, int P>
+__global__ __launch_bounds__(THREADS<W>) void add_norm_backward_kernel(NormBwdArgs a, int nv)
+{
+    __shared__ float red[2 * W];
+    constexpr int E = VEC<T>;
+    const int tid = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+    float dg[P][E], gv[P][E];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        const int c = tid + p * 64 * W;
+#pragma unroll
+        for (int e = 0; e < E; ++e) dg[p][e] = gv[p][e] = 0.0f;
+        if (c < nv) load_vec<T>(static_cast<const T *>(a.g) + (long)c * E, gv[p]);
+    }
+    for (long row = (long)blockIdx.x * ROWS<W> + (W == 1 ? threadIdx.x >> 6 : 0); row < a.rows;
+         row += (long)gridDim.x * ROWS<W>) {
+        const T *dy = static_cast<const T *>(a.dy) + row * a.ldy;
+        const T *sum = static_cast<const T *>(a.sum) + row * a.ldr;
+        const T *ds = a.dsum ? static_cast<const T *>(a.dsum) + row * a.ldr : nullptr;
+        float s[P][E], d[P][E], u[P][E];
+        Sum2 r{0.0f, 0.0f};
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int c = tid + p * 64 * W;
+#pragma unroll
+            for (int e = 0; e < E; ++e) s[p][e] = d[p][e] = u[p][e] = 0.0f;
+            if (c >= nv) continue;
+            load_vec<T>(sum + (long)c * E, s[p]);
+            load_vec<T>(dy + (long)c * E, d[p]);
+            if (ds) load_vec<T>(ds + (long)c * E, u[p]);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                r.a += s[p][e] * s[p][e];
+                r.b += gv[p][e] * d[p][e] * s[p][e];
+            }
+        }
+        r = reduce_row<W, false>(r, red);
+        const float rho = rsqrtf(r.a / (float)(nv * E) + a.eps);
+        const float k = rho * rho * rho * (r.b / (float)(nv * E));
+        T *dx = static_cast<T *>(a.dx) + row * a.ldx;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int c = tid + p * 64 * W;
+            if (c >= nv) continue;
+            float o[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                o[e] = u[p][e] + rho * gv[p][e] * d[p][e] - s[p][e] * k;
+                dg[p][e] += d[p][e] * s[p][e] * rho;
+            }
+            store_vec<T>(dx + (long)c * E, o);
+        }
+    }
+    // one row of sums per wave group
+    const long D = (long)nv * E;
+    float *out = a.partial + ((long)blockIdx.x * ROWS<W> + (W == 1 ? threadIdx.x >> 6 : 0)) * D;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        const int c = tid + p * 64 * W;
+        if (c >= nv) continue;
+#pragma unroll
+        for (int e = 0; e < E; ++e) out[(long)c * E + e] = dg[p][e];
+    }
+}
+
+// Blocks of the backward pass: each leaves ROWS<W> rows of partial sums.
+constexpr int BWD_SLOTS = 1024;   // rows of partial sums at most
+
+int bwd_blocks(long rows, int rows_per_block)
+{
+    const long need = (rows + rows_per_block - 1) / rows_per_block, most = BWD_SLOTS / rows_per_block;
+    return (int)(need < most ? need : most);
+}
+
+template <typename T, int W, int P>
+hipError_t launch_norm(const NormArgs &a, hipStream_t s)
+{
+    const int nv = a.D / VEC<T>;
+    const long need = (a.rows + ROWS<W> - 1) / ROWS<W>;
+    const dim3 grid((unsigned)(need < 65536 ? need : 65536)), block(THREADS<W>);
+    if (a.scale)
+        hipLaunchKernelGGL((add_norm_kernel<T, W, P, true>), grid, block, 0, s, a, nv);
+    else
+        hipLaunchKernelGGL((add_norm_kernel<T, W, P, false>), grid, block, 0, s, a, nv);
+    return hipGetLastError();
+}
+
+template <typename T, int W, int P>
+hipError_t launch_norm_bwd(const NormBwdArgs &a, hipStream_t s)
+{
+    const int blocks = bwd_blocks(a.rows, ROWS<W>);
+    hipLaunchKernelGGL((add_norm_backward_kernel<T, W, P>), dim3(blocks), dim3(THREADS<W>), 0, s, a, a.D / VEC<T>);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    return sum_rows(a.partial, blocks * ROWS<W>, a.D, a.dg, a.accumulate, s);
+}
+
+// Waves and vectors per thread of a row of nv vectors.
+#define NORM_BY_WIDTH(CALL)                    \
+    if (nv <= 64) return CALL(1, 1);           \
+    if (nv <= 128) return CALL(1, 2);          \
+    if (nv <= 256) return CALL(1, 4);          \
+    if (nv <= 512) return CALL(4, 2);          \
+    if (nv <= 1024) return CALL(4, 4);         \
+    if (nv <= 2048) return CALL(8, 4);         \
+    return CALL(16, 4);
+
+template <typename T>
+hipError_t add_norm_t(const NormArgs &a, hipStream_t s)
+{
+    const int nv = a.D / VEC<T>;
+#define CALL(W, P) launch_norm<T, W, P>(a, s)
+    NORM_BY_WIDTH(CALL)
+#undef CALL
+}
+
+template <typename T>
+hipError_t add_norm_backward_t(const NormBwdArgs &a, hipStream_t s)
+{
+    const int nv = a.D / VEC<T>;
+#define CALL(W, P) launch_norm_bwd<T, W, P>(a, s)
+    NORM_BY_WIDTH(CALL)
+#undef CALL
+}
+
+}  // namespace
+
+hipError_t add_norm(DType t, const NormArgs &a, hipStream_t s)
+{
+    if (a.rows == 0) return hipSuccess;
+    const double n = (double)a.rows * a.D;
+    ProfScope ps(K_NORM, s, 0.0, n * (dsize(t) * (1.0 + (a.res ? 1 : 0) + (a.sum ? 1 : 0)) + (a.scale ? 1 : dsize(t))));
+    return t == DType::BF16 ? add_norm_t<bf16_t>(a, s) : add_norm_t<float>(a, s);
+}
+
+size_t norm_partial_floats(long rows, int D) { return (size_t)(rows < BWD_SLOTS ? rows + 3 : BWD_SLOTS) * D; }
+
+hipError_t add_norm_backward(DType t, const NormBwdArgs &a, hipStream_t s)
+{
+    const double n = (double)a.rows * a.D;
+    ProfScope ps(K_NORM, s, 0.0, n * dsize(t) * (a.dsum ? 4.0 : 3.0));
+    if (a.rows == 0) return a.accumulate ? hipSuccess : fill_u32(a.dg, a.D, 0u, s);
+    return t == DType::BF16 ? add_norm_backward_t<bf16_t>(a, s) : add_norm_backward_t<float>(a, s);
+}
+
+}  // namespace lstm355

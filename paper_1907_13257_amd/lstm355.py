@@ -31,6 +31,12 @@ class lstm_kernel_stat_t(ctypes.Structure):
                 ("flops", ctypes.c_double), ("bytes", ctypes.c_double)]
 
 
+class lstm_linattn_desc_t(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int), ("B", ctypes.c_int), ("N", ctypes.c_int), ("K", ctypes.c_int),
+                ("M", ctypes.c_int), ("dtype", ctypes.c_int), ("scale", ctypes.c_float),
+                ("ldq", ctypes.c_long), ("ldk", ctypes.c_long), ("ldv", ctypes.c_long), ("ldo", ctypes.c_long)]
+
+
 class LSTMError(RuntimeError):
     def __init__(self, status: int, where: str, detail: str):
         super().__init__(f"{where}: status {status} ({detail})")
@@ -49,7 +55,8 @@ def load_library():
         raise ImportError(f"{LIB_PATH} is missing: run `python -m paper_1907_13257_amd.build` "
                           "(there is no fallback implementation)")
     lib = ctypes.CDLL(LIB_PATH)
-    vp, i, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+    vp, i, sz, lg, fl = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_long, ctypes.c_float
+    LA = ctypes.POINTER(lstm_linattn_desc_t)
     H = ctypes.c_void_p  # lstm_handle_t
     sig = {
         "lstm_create": ([ctypes.POINTER(lstm_desc_t), ctypes.POINTER(H)], i),
@@ -67,6 +74,17 @@ def load_library():
         "lstm_last_error_detail": ([], ctypes.c_char_p),
         "lstm_describe_tiling": ([H, ctypes.POINTER(ctypes.c_int)], i),
         "lstm_add": ([i, sz, vp, vp, vp, vp], i),
+        "lstm_embed_forward": ([i, lg, lg, i, vp, vp, fl, vp, lg, vp], i),
+        "lstm_embed_workspace_size": ([lg, lg, i], sz),
+        "lstm_embed_backward": ([i, lg, lg, i, vp, vp, lg, fl, vp, i, vp, sz, vp], i),
+        "lstm_add_norm": ([i, lg, i, vp, lg, vp, lg, vp, fl, vp, vp, lg, vp], i),
+        "lstm_add_norm_q8": ([i, lg, i, vp, lg, vp, lg, vp, fl, vp, vp, vp, vp], i),
+        "lstm_add_norm_workspace_size": ([lg, i], sz),
+        "lstm_add_norm_backward": ([i, lg, i, vp, lg, vp, vp, lg, vp, fl, vp, lg, vp, i, vp, sz, vp], i),
+        "lstm_linattn_workspace_size": ([LA], sz),
+        "lstm_linattn_forward": ([LA] + [vp] * 9 + [sz, vp], i),
+        "lstm_linattn_backward": ([LA] + [vp] * 13 + [sz, vp], i),
+        "lstm_linattn_step": ([LA] + [vp] * 9, i),
         "lstm_profile_enable": ([i], i),
         "lstm_profile_reset": ([], i),
         "lstm_profile_read": ([ctypes.POINTER(lstm_kernel_stat_t), i, ctypes.POINTER(i)], i),
@@ -238,6 +256,79 @@ def lstm_add(dtype, n, a, b, out, stream=None):
                                    _stream(stream)), "lstm_add")
 
 
+def _dtype_code(dtype) -> int:
+    if dtype not in ("bf16", "f32"):
+        raise ValueError(f"dtype must be 'bf16' or 'f32', got {dtype!r}")
+    return LSTM_BF16 if dtype == "bf16" else LSTM_F32
+
+
+def lstm_embed_forward(dtype, N, V, D, ids, table, scale, out, ldo=0, stream=None):
+    _check(load_library().lstm_embed_forward(_dtype_code(dtype), N, V, D, _ptr(ids), _ptr(table), scale, _ptr(out),
+                                             ldo, _stream(stream)), "lstm_embed_forward")
+
+
+def lstm_embed_workspace_size(N, V, D) -> int:
+    return load_library().lstm_embed_workspace_size(N, V, D)
+
+
+def lstm_embed_backward(dtype, N, V, D, ids, dout, scale, dtable, accumulate, workspace, ldo=0, stream=None,
+                        workspace_bytes=None):
+    _check(load_library().lstm_embed_backward(_dtype_code(dtype), N, V, D, _ptr(ids), _ptr(dout), ldo, scale,
+                                              _ptr(dtable), int(bool(accumulate)), _ptr(workspace),
+                                              _nbytes(workspace, workspace_bytes), _stream(stream)),
+           "lstm_embed_backward")
+
+
+def lstm_add_norm(dtype, rows, D, x, res, g, eps, sum, y, ldx=0, ldr=0, ldy=0, stream=None):
+    _check(load_library().lstm_add_norm(_dtype_code(dtype), rows, D, _ptr(x), ldx, _ptr(res), ldr, _ptr(g), eps,
+                                        _ptr(sum), _ptr(y), ldy, _stream(stream)), "lstm_add_norm")
+
+
+def lstm_add_norm_q8(dtype, rows, D, x, res, g, eps, sum, y8, scale, ldx=0, ldr=0, stream=None):
+    _check(load_library().lstm_add_norm_q8(_dtype_code(dtype), rows, D, _ptr(x), ldx, _ptr(res), ldr, _ptr(g), eps,
+                                           _ptr(sum), _ptr(y8), _ptr(scale), _stream(stream)), "lstm_add_norm_q8")
+
+
+def lstm_add_norm_workspace_size(rows, D) -> int:
+    return load_library().lstm_add_norm_workspace_size(rows, D)
+
+
+def lstm_add_norm_backward(dtype, rows, D, dy, dsum, sum, g, eps, dx, dg, accumulate, workspace, ldx=0, ldr=0, ldy=0,
+                           stream=None, workspace_bytes=None):
+    _check(load_library().lstm_add_norm_backward(_dtype_code(dtype), rows, D, _ptr(dy), ldy, _ptr(dsum), _ptr(sum),
+                                                 ldr, _ptr(g), eps, _ptr(dx), ldx, _ptr(dg), int(bool(accumulate)),
+                                                 _ptr(workspace), _nbytes(workspace, workspace_bytes),
+                                                 _stream(stream)), "lstm_add_norm_backward")
+
+
+def lstm_linattn_desc(T, B, N, K, M, dtype="bf16", scale=1.0, ldq=0, ldk=0, ldv=0, ldo=0) -> lstm_linattn_desc_t:
+    return lstm_linattn_desc_t(T, B, N, K, M, _dtype_code(dtype), scale, ldq, ldk, ldv, ldo)
+
+
+def lstm_linattn_workspace_size(desc) -> int:
+    return load_library().lstm_linattn_workspace_size(ctypes.byref(desc))
+
+
+def lstm_linattn_forward(desc, q, k, v, decay, lengths, S0, o, ST, workspace, stream=None, workspace_bytes=None):
+    _check(load_library().lstm_linattn_forward(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(decay),
+                                               _ptr(lengths), _ptr(S0), _ptr(o), _ptr(ST), _ptr(workspace),
+                                               _nbytes(workspace, workspace_bytes), _stream(stream)),
+           "lstm_linattn_forward")
+
+
+def lstm_linattn_backward(desc, do, q, k, v, decay, lengths, S0, dST, dq, dk, dv, dS0, workspace, stream=None,
+                          workspace_bytes=None):
+    _check(load_library().lstm_linattn_backward(ctypes.byref(desc), _ptr(do), _ptr(q), _ptr(k), _ptr(v), _ptr(decay),
+                                                _ptr(lengths), _ptr(S0), _ptr(dST), _ptr(dq), _ptr(dk), _ptr(dv),
+                                                _ptr(dS0), _ptr(workspace), _nbytes(workspace, workspace_bytes),
+                                                _stream(stream)), "lstm_linattn_backward")
+
+
+def lstm_linattn_step(desc, q, k, v, decay, lengths, S, S_out, o, stream=None):
+    _check(load_library().lstm_linattn_step(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(decay), _ptr(lengths),
+                                            _ptr(S), _ptr(S_out), _ptr(o), _stream(stream)), "lstm_linattn_step")
+
+
 def lstm_profile_enable(on: bool):
     _check(load_library().lstm_profile_enable(int(bool(on))), "lstm_profile_enable")
 
@@ -309,9 +400,210 @@ class Layer:
         return lstm_describe_tiling(self.handle)
 
 
+def _rows_ptr(t, what, dtype, rows, width, ld, device, optional=False):
+    """The address of a tensor that holds `rows` rows of `width` elements,
+    `ld` elements apart, after checking that it does (its leading dimensions
+    are the rows, however many there are)."""
+    if t is None:
+        if optional:
+            return None
+        raise ValueError(f"{what} is required")
+    if isinstance(t, int):
+        return t
+    if t.dtype is not dtype:
+        raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, the operator on {device}")
+    shape = t.shape
+    if len(shape) == 2:
+        # the common case: one check per property
+        if (shape[0] == rows and shape[1] == width and (width == 1 or t.stride(1) == 1)
+                and (rows <= 1 or t.stride(0) == ld)):
+            return t.data_ptr()
+    n, expect = 1, ld
+    ok = bool(shape) and shape[-1] == width and (width == 1 or t.stride(-1) == 1)
+    for dim in range(len(shape) - 2, -1, -1):
+        ok = ok and (shape[dim] == 1 or t.stride(dim) == expect)
+        n *= shape[dim]
+        expect *= shape[dim]
+    if not ok or n != rows:
+        raise ValueError(f"{what} must be {rows} rows of {width} elements, {ld} apart: got shape {tuple(shape)}, "
+                         f"strides {t.stride()}")
+    return t.data_ptr()
+
+
+class _Operator:
+    """What the operators' classes share: the device they were made on, their
+    workspace, and the stream of a call.  Calls of one object that overlap (on
+    several streams) would share its workspace: order them, or make an object
+    for each."""
+
+    def __init__(self, dtype, device, workspace_bytes):
+        import torch
+        self.code = _dtype_code(dtype)
+        self.dtype, self.torch_dtype = dtype, torch_dtype(dtype)
+        self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise ValueError(f"the operators run on a GPU, not on {self.device}")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._current = torch.cuda.current_device
+        self._float, self._int32, self._int64 = torch.float32, torch.int32, torch.int64
+        self.workspace = torch.empty(workspace_bytes, dtype=torch.uint8, device=self.device)
+        self.ws_ptr, self.ws_bytes = (self.workspace.data_ptr() if workspace_bytes else None), workspace_bytes
+        self.lib = load_library()
+
+    def _stream(self, stream):
+        if self._current() != self.device.index:
+            raise ValueError(f"the operator is on {self.device}, the current device is cuda:{self._current()}")
+        return _stream(stream)
+
+    def _rows(self, t, what, rows, width, ld=None, optional=False):
+        return _rows_ptr(t, what, self.torch_dtype, rows, width, width if ld is None else ld, self.device, optional)
+
+    def _f32(self, t, what, rows, width, optional=False):
+        return _rows_ptr(t, what, self._float, rows, width, width, self.device, optional)
+
+    def _vector(self, t, what, dtype, n, optional=False):
+        if t is None and optional:
+            return None
+        if t is not None and not isinstance(t, int) and (t.numel() != n or not t.is_contiguous()):
+            raise ValueError(f"{what} must be {n} contiguous elements, got shape {tuple(t.shape)}")
+        return _rows_ptr(t if t is None or isinstance(t, int) else t.view(-1), what, dtype, 1, n, n, self.device)
+
+
+class Embedding(_Operator):
+    """Rows of a table [V][D] for N tokens (any leading shape, e.g. [T][B]),
+    scaled, and the table's fp32 gradient.  Tokens outside 0 .. V-1 are
+    padding: rows of zeros, no gradient."""
+
+    def __init__(self, N, V, D, dtype="bf16", scale=1.0, ldo=0, device="cuda"):
+        super().__init__(dtype, device, lstm_embed_workspace_size(N, V, D))
+        self.N, self.V, self.D, self.scale, self.ldo = N, V, D, float(scale), ldo or D
+
+    def forward(self, ids, table, out, stream=None):
+        _check(self.lib.lstm_embed_forward(self.code, self.N, self.V, self.D,
+                                           self._vector(ids, "ids", self._int64, self.N),
+                                           self._rows(table, "table", self.V, self.D), self.scale,
+                                           self._rows(out, "out", self.N, self.D, self.ldo), self.ldo,
+                                           self._stream(stream)), "lstm_embed_forward")
+
+    def backward(self, ids, dout, dtable, accumulate=False, stream=None):
+        _check(self.lib.lstm_embed_backward(self.code, self.N, self.V, self.D,
+                                            self._vector(ids, "ids", self._int64, self.N),
+                                            self._rows(dout, "dout", self.N, self.D, self.ldo), self.ldo, self.scale,
+                                            self._f32(dtable, "dtable", self.V, self.D), int(bool(accumulate)),
+                                            self.ws_ptr, self.ws_bytes, self._stream(stream)), "lstm_embed_backward")
+
+
+class AddNorm(_Operator):
+    """Residual addition and root-mean-square norm of `rows` rows of D values:
+    sum = x + res, y = sum * g / rms(sum), with y in the storage type
+    (`forward`, `backward`) or in e4m3 with a scale per row (`forward_q8`)."""
+
+    def __init__(self, rows, D, dtype="bf16", eps=1e-5, ldx=0, ldr=0, ldy=0, device="cuda"):
+        super().__init__(dtype, device, lstm_add_norm_workspace_size(rows, D))
+        import torch
+        self.rows, self.D, self.eps = rows, D, float(eps)
+        self.ldx, self.ldr, self.ldy = ldx or D, ldr or D, ldy or D
+        self._eight = (torch.float8_e4m3fn, torch.uint8)
+
+    def forward(self, x, res, g, sum, y, stream=None):
+        R, D = self.rows, self.D
+        _check(self.lib.lstm_add_norm(self.code, R, D, self._rows(x, "x", R, D, self.ldx), self.ldx,
+                                      self._rows(res, "res", R, D, self.ldr, True), self.ldr,
+                                      self._vector(g, "g", self.torch_dtype, D), self.eps,
+                                      self._rows(sum, "sum", R, D, self.ldr, True),
+                                      self._rows(y, "y", R, D, self.ldy), self.ldy, self._stream(stream)),
+               "lstm_add_norm")
+
+    def forward_q8(self, x, res, g, sum, y8, scale, stream=None):
+        R, D = self.rows, self.D
+        eight = self._eight[1] if getattr(y8, "dtype", None) is self._eight[1] else self._eight[0]
+        _check(self.lib.lstm_add_norm_q8(self.code, R, D, self._rows(x, "x", R, D, self.ldx), self.ldx,
+                                         self._rows(res, "res", R, D, self.ldr, True), self.ldr,
+                                         self._vector(g, "g", self.torch_dtype, D), self.eps,
+                                         self._rows(sum, "sum", R, D, self.ldr, True),
+                                         _rows_ptr(y8, "y8", eight, R, D, D, self.device),
+                                         self._vector(scale, "scale", self._float, R), self._stream(stream)),
+               "lstm_add_norm_q8")
+
+    def backward(self, dy, dsum, sum, g, dx, dg, accumulate=False, stream=None):
+        R, D = self.rows, self.D
+        _check(self.lib.lstm_add_norm_backward(self.code, R, D, self._rows(dy, "dy", R, D, self.ldy), self.ldy,
+                                               self._rows(dsum, "dsum", R, D, self.ldr, True),
+                                               self._rows(sum, "sum", R, D, self.ldr), self.ldr,
+                                               self._vector(g, "g", self.torch_dtype, D), self.eps,
+                                               self._rows(dx, "dx", R, D, self.ldx), self.ldx,
+                                               self._vector(dg, "dg", self._float, D), int(bool(accumulate)),
+                                               self.ws_ptr, self.ws_bytes, self._stream(stream)),
+               "lstm_add_norm_backward")
+
+
+class LinearAttention(_Operator):
+    """A recurrent layer of linear attention with one decay per head:
+    S_t = decay S_{t-1} + k_t v_t^T, o_t = scale q_t S_t (scale defaults to
+    1 / sqrt(K)).  q, k [T][B][heads*K], v, o [T][B][heads*M], states
+    [B][heads][K][M] fp32, decay [heads] fp32, lengths [B] int32 or None.
+    `step` takes one token of every row (T = 1)."""
+
+    def __init__(self, T, B, heads, K, M, dtype="bf16", scale=None, ldq=0, ldk=0, ldv=0, ldo=0, device="cuda"):
+        scale = K ** -0.5 if scale is None else float(scale)
+        self.desc = lstm_linattn_desc(T, B, heads, K, M, dtype, scale, ldq, ldk, ldv, ldo)
+        super().__init__(dtype, device, lstm_linattn_workspace_size(self.desc))
+        self.T, self.B, self.heads, self.K, self.M, self.scale = T, B, heads, K, M, scale
+        self.ldq, self.ldk = ldq or heads * K, ldk or heads * K
+        self.ldv, self.ldo = ldv or heads * M, ldo or heads * M
+        self._desc = ctypes.byref(self.desc)
+
+    def _state(self, t, what, optional=True):
+        if t is not None and not isinstance(t, int) and not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous")
+        return self._f32(t, what, self.B * self.heads * self.K, self.M, optional)
+
+    def _inputs(self, q, k, v, decay):
+        rows, hk, hm = self.T * self.B, self.heads * self.K, self.heads * self.M
+        return (self._rows(q, "q", rows, hk, self.ldq), self._rows(k, "k", rows, hk, self.ldk),
+                self._rows(v, "v", rows, hm, self.ldv), self._vector(decay, "decay", self._float, self.heads))
+
+    def forward(self, q, k, v, decay, o, lengths=None, S0=None, ST=None, stream=None):
+        _check(self.lib.lstm_linattn_forward(self._desc, *self._inputs(q, k, v, decay),
+                                             self._vector(lengths, "lengths", self._int32, self.B, True),
+                                             self._state(S0, "S0"),
+                                             self._rows(o, "o", self.T * self.B, self.heads * self.M, self.ldo),
+                                             self._state(ST, "ST"), self.ws_ptr, self.ws_bytes, self._stream(stream)),
+               "lstm_linattn_forward")
+
+    def backward(self, do, q, k, v, decay, dq, dk, dv, lengths=None, S0=None, dST=None, dS0=None, stream=None):
+        rows, hk, hm = self.T * self.B, self.heads * self.K, self.heads * self.M
+        _check(self.lib.lstm_linattn_backward(self._desc, self._rows(do, "do", rows, hm, self.ldo),
+                                              *self._inputs(q, k, v, decay),
+                                              self._vector(lengths, "lengths", self._int32, self.B, True),
+                                              self._state(S0, "S0"), self._state(dST, "dST"),
+                                              self._rows(dq, "dq", rows, hk, self.ldq, True),
+                                              self._rows(dk, "dk", rows, hk, self.ldk, True),
+                                              self._rows(dv, "dv", rows, hm, self.ldv, True),
+                                              self._state(dS0, "dS0"), self.ws_ptr, self.ws_bytes,
+                                              self._stream(stream)), "lstm_linattn_backward")
+
+    def step(self, q, k, v, decay, S, S_out, o, lengths=None, stream=None):
+        _check(self.lib.lstm_linattn_step(self._desc, *self._inputs(q, k, v, decay),
+                                          self._vector(lengths, "lengths", self._int32, self.B, True),
+                                          self._state(S, "S", False), self._state(S_out, "S_out", False),
+                                          self._rows(o, "o", self.T * self.B, self.heads * self.M, self.ldo),
+                                          self._stream(stream)), "lstm_linattn_step")
+
+
 class StackLayer:
-    def __init__(self, I, H, Hp=0, bidirectional=False, residual=False):
-        self.I, self.H, self.Hp, self.bidirectional, self.residual = I, H, Hp, bidirectional, residual
+    """A layer of a Stack.  residual: its output is y plus the residual stream
+    (for a layer without norms below it, its own input).  norm (residual layers
+    only): the sum goes on as the residual stream and its root-mean-square norm
+    with the gain params["g"] is what the next layer reads."""
+
+    def __init__(self, I, H, Hp=0, bidirectional=False, residual=False, norm=False):
+        self.I, self.H, self.Hp, self.bidirectional, self.residual, self.norm = I, H, Hp, bidirectional, residual, norm
+        if norm and not residual:
+            raise ValueError("a layer with a norm is a residual layer")
         self.Hr = Hp if Hp else H
         self.out = self.Hr * (2 if bidirectional else 1)
 
@@ -322,11 +614,17 @@ class Stack:
     2*Hr); a residual layer's output is y + x (lstm_add).  Backward mirrors it:
     the directions' input gradients and the identity path are summed with
     lstm_add.  Initial states are zero and the final states get no gradient.
+    A residual layer with a norm hands its sum on as the residual stream of the
+    layers above and the norm of the sum as their input (lstm_add_norm).  With
+    `vocab` rows of an embedding the stack's input is token ids [T][B] and a
+    table [vocab][I], its rows scaled by embed_scale.
 
     params[l][d] = dict(W, R, b[, P]) device tensors; grads likewise with
-    dW, dR, db[, dP] (fp32), allocated here."""
+    dW, dR, db[, dP] (fp32), allocated here.  params[l][0]["g"] and
+    grads[l][0]["dg"]: the gain of a layer's norm."""
 
-    def __init__(self, T, B, layers: Sequence[StackLayer], dtype="bf16", device="cuda", wavefront=True):
+    def __init__(self, T, B, layers: Sequence[StackLayer], dtype="bf16", device="cuda", wavefront=True, vocab=0,
+                 embed_scale=1.0, eps=1e-5):
         import torch
         self.T, self.B, self.dtype, self.device = T, B, dtype, device
         self.wavefront = wavefront
@@ -358,6 +656,13 @@ class Stack:
         self.dxbuf = [[torch.empty((T, B, L.I), dtype=td, device=device) for _ in range(2 if L.bidirectional else 1)]
                       for L in self.layers]
         self.gbuf = [torch.empty((T, B, L.I), dtype=td, device=device) for L in self.layers]
+        self.norms = [AddNorm(T * B, L.out, dtype, eps, device=device) if L.norm else None for L in self.layers]
+        self.nout = [torch.empty((T, B, L.out), dtype=td, device=device) if L.norm else None for L in self.layers]
+        self.dsum = [torch.empty((T, B, L.out), dtype=td, device=device) if L.norm else None for L in self.layers]
+        self.embedding = self.rows = self.ids = None
+        if vocab:
+            self.embedding = Embedding(T * B, vocab, self.layers[0].I, dtype, embed_scale, device=device)
+            self.rows = torch.empty((T, B, self.layers[0].I), dtype=td, device=device)
 
     def alloc_grads(self, params):
         import torch
@@ -370,17 +675,23 @@ class Stack:
                          db=torch.empty(p["b"].shape, dtype=torch.float32, device=self.device))
                 if L.Hp:
                     g["dP"] = torch.empty(p["P"].shape, dtype=torch.float32, device=self.device)
+                if "g" in p:
+                    g["dg"] = torch.empty(p["g"].shape, dtype=torch.float32, device=self.device)
                 gl.append(g)
             grads.append(gl)
         return grads
 
-    def forward(self, x, params, stream=None):
+    def forward(self, x, params, stream=None, table=None):
+        if self.embedding is not None:
+            self.ids = x
+            self.embedding.forward(x, table, self.rows, stream)
+            x = self.rows
         # a stack of unidirectional LSTM layers (residual ones included) runs
         # as one layer wavefront when the library supports its shape
         # (lstm_forward_stack)
         self.last_forward = "layers"
         if (self.wavefront and 2 <= len(self.layers) <= 4 and self.dtype == "bf16"
-                and all(not L.bidirectional and not L.Hp for L in self.layers)):
+                and all(not L.bidirectional and not L.Hp and not L.norm for L in self.layers)):
             lays = [d[0] for d in self.dirs]
             residual = [L.residual for L in self.layers]
             if lstm_forward_stack([l.handle for l in lays], x, [p[0]["W"] for p in params],
@@ -391,7 +702,7 @@ class Stack:
                 self.inputs = [x] + outs[:-1]
                 self.last_forward = "wavefront"
                 return outs[-1]
-        cur = x
+        cur = carry = x   # the layer's input, and the residual stream beside it
         for li, L in enumerate(self.layers):
             self.inputs[li] = cur
             y = self.y[li]
@@ -399,14 +710,27 @@ class Stack:
                 p = params[li][d]
                 yd = y[:, :, d * L.Hr:] if d else y
                 lay.forward(cur, p["W"], p["R"], p["b"], p.get("P"), y=yd, stream=stream)
-            if L.residual:
-                lstm_add(self.dtype, y.numel(), y, cur, self.xout[li], stream)
-                cur = self.xout[li]
+            if L.norm:
+                self.norms[li].forward(y, carry, params[li][0]["g"], self.xout[li], self.nout[li], stream)
+                cur, carry = self.nout[li], self.xout[li]
+            elif L.residual:
+                lstm_add(self.dtype, y.numel(), y, carry, self.xout[li], stream)
+                cur = carry = self.xout[li]
             else:
-                cur = y
+                cur = carry = y
         return cur
 
-    def backward(self, d_out, params, grads, accumulate=False, stream=None):
+    def backward(self, d_out, params, grads, accumulate=False, stream=None, dtable=None):
+        """Gradients of the layers, and of the embedding's table into `dtable`
+        where there is one; returns the gradient of the first layer's input."""
+        if self.embedding is not None and dtable is None:
+            raise ValueError("dtable is required: the stack has an embedding")
+        dx = self._backward_layers(d_out, params, grads, accumulate, stream)
+        if self.embedding is not None:
+            self.embedding.backward(self.ids, dx, dtable, accumulate, stream)
+        return dx
+
+    def _backward_layers(self, d_out, params, grads, accumulate, stream):
         # after a wavefront forward, the backward runs as one too when its
         # shapes allow (lstm_backward_stack)
         self.last_backward = "layers"
@@ -426,11 +750,15 @@ class Stack:
                                        residual=[L.residual for L in self.layers], sums=self.xout):
                     self.last_backward = "wavefront"
                     return dx
-        g = d_out
+        g, gc = d_out, None   # gradients of the layer's output and, past a norm, of the residual stream
         for li in range(len(self.layers) - 1, -1, -1):
             L = self.layers[li]
             x = self.inputs[li]
             y = self.y[li]
+            if L.norm:
+                self.norms[li].backward(g, gc, self.xout[li], params[li][0]["g"], self.dsum[li], grads[li][0]["dg"],
+                                        accumulate, stream)
+                g = self.dsum[li]
             for d, lay in enumerate(self.dirs[li]):
                 p = params[li][d]
                 off = d * L.Hr
@@ -442,10 +770,13 @@ class Stack:
             if L.bidirectional:
                 lstm_add(self.dtype, dx.numel(), dx, self.dxbuf[li][1], out, stream)
                 dx = out
+            if li > 0 and self.layers[li - 1].norm:
+                g, gc = dx, (g if L.residual else None)
+                continue
             if L.residual:
                 lstm_add(self.dtype, dx.numel(), dx, g, out, stream)
                 dx = out
-            g = dx
+            g, gc = dx, None
         return g
 
     def check(self, stream=None) -> int:

@@ -60,12 +60,84 @@ __global__ __launch_bounds__(256) void embed_forward_kernel(long N, long V, int 
 }
 
 // ---------------------------------------------------------------------------
-// The tokens sorted by table row, position by position within a row: a stable
-// radix sort of (row, position), least significant digit first.  The key of a
-// token outside the table is V, behind every row.  A pass is a count of each
-// block's digits and a scatter; a block owns `span` consecutive tokens.
+// The tokens sorted by table row, position by position within a row.  The key
+// of a token outside the table is V, behind every row.  Every launch of the
+// sort takes a share of the work beside it that needs no order: the zeros of an
+// overwritten gradient, written by blocks behind the sorting ones, so that the
+// sort's few blocks and their latency hide behind those stores.
 // ---------------------------------------------------------------------------
-constexpr int SORT_TILE = 1024;        // tokens sorted at a time by a block, one per thread
+constexpr int SORT_TILE = 1024;        // threads of a sorting block, tokens sorted at a time
+
+struct Fill {
+    f32x4 *p;
+    long n;      // zeros p[0 .. n)
+    int first;   // number of sorting blocks
+};
+
+// Whether this block writes zeros (and has).
+__device__ __forceinline__ bool fill_block(const Fill &f)
+{
+    if ((int)blockIdx.x < f.first) return false;
+    const long step = (long)(gridDim.x - f.first) * SORT_TILE;
+    for (long i = (long)(blockIdx.x - f.first) * SORT_TILE + threadIdx.x; i < f.n; i += step)
+        f.p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    return true;
+}
+
+__device__ __forceinline__ unsigned token_key(const int64_t *ids, const unsigned *keys, long i, long V)
+{
+    if (keys) return keys[i];
+    const int64_t id = ids[i];
+    return id >= 0 && id < V ? (unsigned)id : (unsigned)V;
+}
+
+// Few tokens: a token's place is the number of keys before its own, counted
+// outright.  A block places 64 tokens, one per lane; each of its 16 waves
+// compares them with a sixteenth of all keys.
+constexpr int RANK_MAX = 8192;
+__global__ __launch_bounds__(SORT_TILE) void rank_kernel(int N, long V, const int64_t *__restrict__ ids,
+                                                         unsigned *__restrict__ keys_out, int *__restrict__ pos_out,
+                                                         Fill fill)
+{
+    __shared__ __align__(16) unsigned keys[RANK_MAX];
+    __shared__ int counts[16][64];
+    if (fill_block(fill)) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    for (int i = tid; i < N; i += SORT_TILE) keys[i] = token_key(ids, nullptr, i, V);
+    __syncthreads();
+    const int i = blockIdx.x * 64 + lane, i0 = blockIdx.x * 64;
+    const unsigned mine = i < N ? keys[i] : 0u;
+    const int per = ((N + 63) / 64 + 15) / 16 * 64;   // keys of a wave, whole groups of 64
+    const int j0 = wave * per, j1 = min(N, j0 + per);
+    int c = 0;
+    // equal keys count if they come first: those of earlier groups do, and in
+    // the token's own group those of lower lanes
+    for (int j = j0; j < min(j1, i0); j += 4) {
+        const u32x4 k = *reinterpret_cast<const u32x4 *>(keys + j);
+        c += (k[0] <= mine) + (k[1] <= mine) + (k[2] <= mine) + (k[3] <= mine);
+    }
+    if (i0 >= j0 && i0 < j1)
+        for (int j = i0; j < min(j1, i0 + 64); ++j) c += keys[j] < mine || (keys[j] == mine && j < i);
+    int j = max(j0, i0 + 64);
+    for (; j + 4 <= j1; j += 4) {
+        const u32x4 k = *reinterpret_cast<const u32x4 *>(keys + j);
+        c += (k[0] < mine) + (k[1] < mine) + (k[2] < mine) + (k[3] < mine);
+    }
+    for (; j < j1; ++j) c += keys[j] < mine;
+    counts[wave][lane] = c;
+    __syncthreads();
+    if (wave == 0 && i < N) {
+        int at = 0;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) at += counts[w][lane];
+        keys_out[at] = mine;
+        pos_out[at] = i;
+    }
+}
+
+// Many tokens: a stable radix sort of (key, position), least significant digit
+// first.  A pass is a count of each block's digits and a scatter; a block owns
+// `span` consecutive tokens.
 constexpr int SORT_MAX_BLOCKS = 256;
 constexpr int SORT_MAX_BITS = 11;      // of a digit: 2048 counters per wave of the block, 64 KiB of LDS
 
@@ -80,7 +152,6 @@ SortPlan sort_plan(long N, long V)
     int keybits = 0;
     while (keybits < 32 && (V >> keybits)) ++keybits;   // keys are 0 .. V
     p.passes = (keybits + SORT_MAX_BITS - 1) / SORT_MAX_BITS;
-    if (p.passes < 1) p.passes = 1;
     p.bits = (keybits + p.passes - 1) / p.passes;
     const long tiles = (N + SORT_TILE - 1) / SORT_TILE;
     const long per = (tiles + SORT_MAX_BLOCKS - 1) / SORT_MAX_BLOCKS;
@@ -89,18 +160,12 @@ SortPlan sort_plan(long N, long V)
     return p;
 }
 
-__device__ __forceinline__ unsigned token_key(const int64_t *ids, const unsigned *keys, long i, long V)
-{
-    if (keys) return keys[i];
-    const int64_t id = ids[i];
-    return id >= 0 && id < V ? (unsigned)id : (unsigned)V;
-}
-
 __global__ __launch_bounds__(SORT_TILE) void sort_count_kernel(long N, long V, const int64_t *__restrict__ ids,
                                                                const unsigned *__restrict__ keys, int shift, int bits,
-                                                               long span, int *__restrict__ hist)
+                                                               long span, int *__restrict__ hist, Fill fill)
 {
     __shared__ int cnt[1 << SORT_MAX_BITS];
+    if (fill_block(fill)) return;
     const int bins = 1 << bits;
     for (int b = threadIdx.x; b < bins; b += SORT_TILE) cnt[b] = 0;
     __syncthreads();
@@ -108,7 +173,7 @@ __global__ __launch_bounds__(SORT_TILE) void sort_count_kernel(long N, long V, c
     for (long i = i0 + threadIdx.x; i < i1; i += SORT_TILE)
         atomicAdd(&cnt[(token_key(ids, keys, i, V) >> shift) & (bins - 1)], 1);
     __syncthreads();
-    for (int b = threadIdx.x; b < bins; b += SORT_TILE) hist[(long)b * gridDim.x + blockIdx.x] = cnt[b];
+    for (int b = threadIdx.x; b < bins; b += SORT_TILE) hist[(long)blockIdx.x * bins + b] = cnt[b];
 }
 
 __global__ __launch_bounds__(SORT_TILE) void sort_scatter_kernel(long N, long V, const int64_t *__restrict__ ids,
@@ -116,27 +181,35 @@ __global__ __launch_bounds__(SORT_TILE) void sort_scatter_kernel(long N, long V,
                                                                  const int *__restrict__ pos, int shift, int bits,
                                                                  long span, const int *__restrict__ hist,
                                                                  unsigned *__restrict__ keys_out,
-                                                                 int *__restrict__ pos_out)
+                                                                 int *__restrict__ pos_out, Fill fill)
 {
     constexpr int WAVES = SORT_TILE / 64;
     __shared__ unsigned short in_wave[WAVES][1 << SORT_MAX_BITS];   // per wave: counts, then counts of earlier waves
     __shared__ int base[1 << SORT_MAX_BITS];                         // next place of each digit
     __shared__ int sums[WAVES];
+    if (fill_block(fill)) return;
     const int bins = 1 << bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int nb = gridDim.x;
+    const int nb = fill.first;
 
     // this block's first place of each digit: all smaller digits, and the
     // digit's tokens in earlier blocks.  Thread t takes digits 2t and 2t + 1.
     int total[2] = {0, 0}, before[2] = {0, 0};
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int b = 2 * tid + j;
-        if (b < bins)
-            for (int k = 0; k < nb; ++k) {
-                const int c = hist[(long)b * nb + k];
-                total[j] += c;
-                if (k < (int)blockIdx.x) before[j] += c;
-            }
+    if (2 * tid < bins) {
+        int k = 0;
+#pragma unroll 8
+        for (; k < (int)blockIdx.x; ++k) {
+            const int2 c = *reinterpret_cast<const int2 *>(hist + (long)k * bins + 2 * tid);
+            before[0] += c.x;
+            before[1] += c.y;
+        }
+        total[0] = before[0];
+        total[1] = before[1];
+#pragma unroll 8
+        for (; k < nb; ++k) {
+            const int2 c = *reinterpret_cast<const int2 *>(hist + (long)k * bins + 2 * tid);
+            total[0] += c.x;
+            total[1] += c.y;
+        }
     }
     int run = total[0] + total[1];
     for (int d = 1; d < 64; d *= 2) {
@@ -147,12 +220,15 @@ __global__ __launch_bounds__(SORT_TILE) void sort_scatter_kernel(long N, long V,
     __syncthreads();
     for (int w = 0; w < wave; ++w) run += sums[w];
     const int first = run - total[0] - total[1];
-    if (2 * tid < bins) base[2 * tid] = first + before[0];
-    if (2 * tid + 1 < bins) base[2 * tid + 1] = first + total[0] + before[1];
+    if (2 * tid < bins) {
+        base[2 * tid] = first + before[0];
+        base[2 * tid + 1] = first + total[0] + before[1];
+    }
 
     const long i0 = blockIdx.x * span, i1 = min(N, i0 + span);
     for (long t0 = i0; t0 < i1; t0 += SORT_TILE) {
-        for (int e = tid; e < WAVES * bins; e += SORT_TILE) in_wave[e >> bits][e & (bins - 1)] = 0;
+        for (int e = tid; e < WAVES * bins / 2; e += SORT_TILE)
+            reinterpret_cast<unsigned *>(&in_wave[2 * e >> bits][0])[e & (bins / 2 - 1)] = 0;
         __syncthreads();
         const long i = t0 + tid;
         const bool on = i < i1;
@@ -193,94 +269,171 @@ __global__ __launch_bounds__(SORT_TILE) void sort_scatter_kernel(long N, long V,
 }
 
 // ---------------------------------------------------------------------------
-// Sums over the sorted tokens.  Equal rows are neighbours, so each run of RUN
-// sorted tokens is summed by one group of threads, whatever the frequencies:
-// a row whose tokens lie within one run is final, a row that reaches over runs
-// leaves a partial sum per run (the first of a run's two slots if it came from
-// the run before, else the second), which embed_combine_kernel adds in order.
+// Sums over the sorted tokens.  Equal rows are neighbours, so the work is cut
+// by tokens, whatever the frequencies: a wave has RUN sorted tokens and 64
+// vectors of the columns.  A row of at most RUN tokens is summed whole by the
+// run its first token lies in; of a longer row every run sums its own tokens
+// and leaves a partial sum (in the first of a run's two slots if the row came
+// from the run before, else in the second), which embed_combine_kernel adds in
+// order.  Whether a row is longer shows in the RUN keys before and behind the
+// run, a lane each, as the bits at which the key changes.
 // ---------------------------------------------------------------------------
 constexpr int RUN = 16;
+
+struct Window {
+    unsigned key;                // lane l: that of sorted token RUN * (r - 1) + l, l < 3 RUN
+    int pos;
+    unsigned long long change;   // bit l: the key of lane l differs from lane l - 1's
+};
+
+__device__ __forceinline__ Window run_window(const unsigned *keys, const int *pos, long N, long r, int lane)
+{
+    const long i = RUN * (r - 1) + lane;
+    const bool in = i >= 0 && i < N && lane < 3 * RUN;
+    Window w;
+    w.key = in ? keys[i] : (i < 0 ? 0xffffffffu : 0xfffffffeu);
+    w.pos = in && pos ? pos[i] : 0;
+    w.change = __ballot(w.key != __shfl_up(w.key, 1));
+    return w;
+}
+
+__device__ __forceinline__ int next_change(const Window &w, int from)   // the first at or behind `from`, 64 if none
+{
+    const unsigned long long m = w.change >> from;
+    return from < 64 && m ? from + __builtin_ctzll(m) : 64;
+}
 
 template <typename T>
 __global__ __launch_bounds__(256) void embed_runs_kernel(long N, long V, int nv, const unsigned *__restrict__ keys,
                                                          const int *__restrict__ pos, const T *__restrict__ dout,
                                                          long ldo, float scale, float *__restrict__ dtable,
-                                                         int accumulate, float *__restrict__ partial, int tpr)
+                                                         int accumulate, float *__restrict__ partial)
 {
-    const long D = (long)nv * VEC<T>, nruns = (N + RUN - 1) / RUN;
-    const long r = (long)blockIdx.x * (256 / tpr) + threadIdx.x / tpr;
-    if (r >= nruns) return;
-    const long i0 = r * RUN, i1 = min(N, i0 + RUN);
-    const unsigned none = (unsigned)V;
-    const unsigned prev = i0 > 0 ? keys[i0 - 1] : none, next = i1 < N ? keys[i1] : none;
-    for (int c = blockIdx.y * tpr + threadIdx.x % tpr; c < nv; c += gridDim.y * tpr) {
+    constexpr int BATCH = 8;     // rows in flight
+    const int lane = threadIdx.x & 63, blocks = (nv + 63) / 64;
+    const long D = (long)nv * VEC<T>, tasks = (N + RUN - 1) / RUN * blocks;
+    for (long task = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); task < tasks;
+         task += (long)gridDim.x * 4) {
+        const long r = task / blocks;
+        const int c = (int)(task % blocks) * 64 + lane;
+        const Window w = run_window(keys, pos, N, r, lane);
+        // tokens p0 .. p1 - 1 of the window
+        int p0 = RUN, p1 = 2 * RUN;
+        if (!(w.change >> RUN & 1)) {   // a row from the run before: this run's if it is longer than RUN
+            const unsigned long long before = w.change & ((1ull << RUN) - 2);
+            const int end = next_change(w, RUN + 1);
+            if (before && end - (63 - __builtin_clzll(before)) <= RUN) p0 = end;
+        }
+        if (p0 >= p1) continue;
+        const int last = 63 - __builtin_clzll((w.change | 1ull << p0) & ((1ull << p1) - 1));   // where the last row starts
+        if (!(w.change >> p1 & 1) && (w.change >> last & 1)) {
+            const int end = next_change(w, p1);
+            if (end - last <= RUN) p1 = end;
+        }
+        // tokens outside the table are behind all others
+        const unsigned long long outside = __ballot(w.key >= (unsigned)V) >> p0;
+        if (outside) p1 = min(p1, p0 + __builtin_ctzll(outside));
+
         float acc[VEC<T>];
 #pragma unroll
         for (int e = 0; e < VEC<T>; ++e) acc[e] = 0.0f;
-        unsigned cur = keys[i0];
-        bool head = cur == prev;
-        auto flush = [&](bool more) {
-            if (cur >= none) return;
-            if (head || more) {
-                float *p = partial + (2 * r + (head ? 0 : 1)) * D + (long)c * VEC<T>;
+        int start = p0;
+        auto flush = [&](int end) {   // the row of tokens start .. end - 1
+            const bool head = !(w.change >> start & 1), more = !(w.change >> end & 1);
+            if (c < nv) {
+                const bool part = head || more;
+                float *p = part ? partial + (2 * r + (head ? 0 : 1)) * D + (long)c * VEC<T>
+                                : dtable + (long)(unsigned)__builtin_amdgcn_readlane(w.key, start) * D + (long)c * VEC<T>;
 #pragma unroll
-                for (int e = 0; e < VEC<T>; ++e) p[e] = acc[e];
-                return;
+                for (int e = 0; e < VEC<T>; e += 4) {
+                    f32x4 v = {acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+                    f32x4 *to = reinterpret_cast<f32x4 *>(p + e);
+                    if (!part) v = accumulate ? *to + scale * v : scale * v;
+                    *to = v;
+                }
             }
-            float *p = dtable + (long)cur * D + (long)c * VEC<T>;
 #pragma unroll
-            for (int e = 0; e < VEC<T>; ++e) p[e] = accumulate ? p[e] + scale * acc[e] : scale * acc[e];
+            for (int e = 0; e < VEC<T>; ++e) acc[e] = 0.0f;
+            start = end;
         };
-        for (long i = i0; i < i1; ++i) {
-            const unsigned k = keys[i];
-            if (k != cur) {
-                flush(false);
-                cur = k;
-                head = false;
+        for (int b = p0; b < p1; b += BATCH) {
+            u32x4 v[BATCH];
 #pragma unroll
-                for (int e = 0; e < VEC<T>; ++e) acc[e] = 0.0f;
+            for (int k = 0; k < BATCH; ++k) {
+                const long row = __builtin_amdgcn_readlane(w.pos, min(b + k, p1 - 1));
+                v[k] = c < nv ? ldg16(dout + row * ldo + (long)c * VEC<T>) : zero16();
             }
-            if (k >= none) break;   // the tokens outside the table are the last
-            float f[VEC<T>];
-            unpack<T>(ldg16(dout + (long)pos[i] * ldo + (long)c * VEC<T>), f);
 #pragma unroll
-            for (int e = 0; e < VEC<T>; ++e) acc[e] += f[e];
+            for (int k = 0; k < BATCH; ++k) {
+                if (b + k >= p1) break;
+                if (b + k > start && (w.change >> (b + k) & 1)) flush(b + k);
+                float f[VEC<T>];
+                unpack<T>(v[k], f);
+#pragma unroll
+                for (int e = 0; e < VEC<T>; ++e) acc[e] += f[e];
+            }
         }
-        flush(cur == next);
+        if (p1 > start) flush(p1);
     }
 }
 
-// Rows that reach over several runs: the block of the run a row starts in adds
-// its partial sums, a quarter of them per group of 64 lanes.
-__global__ __launch_bounds__(256) void embed_combine_kernel(long N, long V, int D, const unsigned *__restrict__ keys,
-                                                            const float *__restrict__ partial, float scale,
-                                                            float *__restrict__ dtable, int accumulate)
+// Rows of more than RUN tokens: a block looks at 16 runs, one per wave, and its
+// waves add the partial sums of every long row that starts in one of them and
+// reaches over its end, a sixteenth each.
+__global__ __launch_bounds__(1024) void embed_combine_kernel(long N, long V, int D, const unsigned *__restrict__ keys,
+                                                             const float *__restrict__ partial, float scale,
+                                                             float *__restrict__ dtable, int accumulate)
 {
-    __shared__ f32x4 part[4][64];
-    const long r = blockIdx.x, i0 = r * RUN, i1 = i0 + RUN;
-    if (i1 >= N) return;
-    const unsigned key = keys[i1 - 1];
-    if (key >= (unsigned)V || keys[i1] != key) return;             // the last row of the run ends with it
-    if (i0 > 0 && keys[i0] == key && keys[i0 - 1] == key) return;  // it started in an earlier run
+    __shared__ long owner_runs[16];
+    __shared__ f32x4 part[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long nruns = (N + RUN - 1) / RUN;
-    long lo = r + 1, hi = nruns;   // the last run that starts with the row: in [lo, hi)
-    while (hi - lo > 1) {
-        const long mid = (lo + hi) / 2;
-        if (keys[mid * RUN] == key) lo = mid; else hi = mid;
-    }
-    const long n = lo - r + 1, per = (n + 3) / 4;   // partial sums in all, and of a group
-    const int lane = threadIdx.x & 63, grp = threadIdx.x >> 6;
     const int c = (blockIdx.y * 64 + lane) * 4;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    if (c < D)
-        for (long j = grp * per; j < min(n, (grp + 1) * per); ++j)
-            acc += *reinterpret_cast<const f32x4 *>(partial + (j == 0 ? 2 * r + 1 : 2 * (r + j)) * D + c);
-    part[grp][lane] = acc;
-    __syncthreads();
-    if (grp == 0 && c < D) {
-        acc = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
-        f32x4 *p = reinterpret_cast<f32x4 *>(dtable + (long)key * D + c);
-        *p = accumulate ? *p + scale * acc : scale * acc;
+    for (long r0 = (long)blockIdx.x * 16; r0 < nruns; r0 += (long)gridDim.x * 16) {
+        long runs = 0;   // that the long row of run `mine` reaches over
+        const long mine = r0 + wave;
+        if (mine < nruns) {
+            const Window w = run_window(keys, nullptr, N, mine, lane);
+            const int last = 63 - __builtin_clzll((w.change | 1) & ((1ull << 2 * RUN) - 1));
+            const unsigned key = __builtin_amdgcn_readlane(w.key, 2 * RUN - 1);
+            if (key < (unsigned)V && last >= RUN && !(w.change >> 2 * RUN & 1) && next_change(w, 2 * RUN) - last > RUN) {
+                // the last run that starts with the row: 64 probes at a time
+                long lo = mine + 1, left = nruns - lo;   // run lo starts with it, run lo + left does not
+                while (left > 1) {
+                    const long step = (left + 63) / 64;
+                    const long at = lo + lane * step;
+                    const int hits = __popcll(__ballot(at < lo + left && keys[min(at, nruns - 1) * RUN] == key));
+                    lo += (hits - 1) * step;
+                    left = min(step, nruns - lo);
+                }
+                runs = lo - mine + 1;
+            }
+        }
+        if (lane == 0) owner_runs[wave] = runs;
+        __syncthreads();
+        for (int o = 0; o < 16; ++o) {
+            const long n = owner_runs[o];
+            if (!n) continue;
+            const long r = r0 + o, per = (n + 15) / 16;
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+            if (c < D) {
+                const long end = min(n, (wave + 1) * per);
+#pragma unroll 8
+                for (long j = wave * per; j < end; ++j)
+                    acc += *reinterpret_cast<const f32x4 *>(partial + (j == 0 ? 2 * r + 1 : 2 * (r + j)) * D + c);
+            }
+            part[wave][lane] = acc;
+            __syncthreads();
+            if (wave == 0 && c < D) {
+                acc = part[0][lane];
+#pragma unroll
+                for (int k = 1; k < 16; ++k) acc += part[k][lane];
+                f32x4 *p = reinterpret_cast<f32x4 *>(dtable + (long)keys[r * RUN + RUN - 1] * D + c);
+                *p = accumulate ? *p + scale * acc : scale * acc;
+            }
+            __syncthreads();
+        }
+        __syncthreads();   // owner_runs has been read
     }
 }
 
@@ -312,37 +465,56 @@ template <typename T>
 hipError_t embed_backward_t(long N, long V, int D, const int64_t *ids, const T *dout, long ldo, float scale,
                             float *dtable, int accumulate, char *ws, hipStream_t s)
 {
-    if (!accumulate) {
-        const hipError_t e = fill_u32(dtable, (size_t)V * D, 0u, s);
-        if (e != hipSuccess) return e;
-    }
-    if (N == 0) return hipSuccess;
     const EmbedWs w = embed_ws(N, V, D);
     const SortPlan p = sort_plan(N, V);
+    const bool few = N <= RANK_MAX;
+    // the zeros, in equal shares of the sort's launches
+    const long zeros = accumulate ? 0 : V * (D / 4);
+    const int launches = few ? 1 : 2 * p.passes;
+    long zeroed = 0;
+    int fill_blocks = 0;
+    auto share = [&](int sort_blocks, int k) {
+        const long upto = zeros * (k + 1) / launches, n = upto - zeroed;
+        const long need = (n + SORT_TILE - 1) / SORT_TILE;
+        fill_blocks = (int)(need < 1024 ? need : 1024);
+        const Fill f{reinterpret_cast<f32x4 *>(dtable) + zeroed, n, sort_blocks};
+        zeroed = upto;
+        return f;
+    };
     unsigned *keys[2] = {reinterpret_cast<unsigned *>(ws + w.keys[0]), reinterpret_cast<unsigned *>(ws + w.keys[1])};
     int *pos[2] = {reinterpret_cast<int *>(ws + w.pos[0]), reinterpret_cast<int *>(ws + w.pos[1])};
     int *hist = reinterpret_cast<int *>(ws + w.hist);
-    float *partial = reinterpret_cast<float *>(ws + w.partial);
     const unsigned *ksrc = nullptr;
     const int *psrc = nullptr;
-    int to = 0;
-    for (int k = 0; k < p.passes; ++k, to ^= 1) {
-        hipLaunchKernelGGL(sort_count_kernel, dim3(p.blocks), dim3(SORT_TILE), 0, s, N, V, ids, ksrc, k * p.bits,
-                           p.bits, p.span, hist);
-        hipLaunchKernelGGL(sort_scatter_kernel, dim3(p.blocks), dim3(SORT_TILE), 0, s, N, V, ids, ksrc, psrc,
-                           k * p.bits, p.bits, p.span, hist, keys[to], pos[to]);
+    if (few) {
+        const int blocks = (int)((N + 63) / 64);
+        const Fill f = share(blocks, 0);
+        if (blocks + fill_blocks)
+            hipLaunchKernelGGL(rank_kernel, dim3(blocks + fill_blocks), dim3(SORT_TILE), 0, s, (int)N, V, ids, keys[0],
+                               pos[0], f);
+        ksrc = keys[0];
+        psrc = pos[0];
+    }
+    for (int k = 0, to = 0; !few && k < p.passes; ++k, to ^= 1) {
+        Fill f = share(p.blocks, 2 * k);
+        hipLaunchKernelGGL(sort_count_kernel, dim3(p.blocks + fill_blocks), dim3(SORT_TILE), 0, s, N, V, ids, ksrc,
+                           k * p.bits, p.bits, p.span, hist, f);
+        f = share(p.blocks, 2 * k + 1);
+        hipLaunchKernelGGL(sort_scatter_kernel, dim3(p.blocks + fill_blocks), dim3(SORT_TILE), 0, s, N, V, ids, ksrc,
+                           psrc, k * p.bits, p.bits, p.span, hist, keys[to], pos[to], f);
         ksrc = keys[to];
         psrc = pos[to];
     }
-    const int nv = D / VEC<T>;
-    int tpr = lanes_per_row(nv);
-    while (tpr < 256 && tpr < nv) tpr *= 2;
-    const long nruns = (N + RUN - 1) / RUN;
-    const int rpb = 256 / tpr;
-    hipLaunchKernelGGL(embed_runs_kernel<T>, dim3((unsigned)((nruns + rpb - 1) / rpb), (nv + tpr - 1) / tpr), dim3(256), 0,
-                       s, N, V, nv, ksrc, psrc, dout, ldo, scale, dtable, accumulate, partial, tpr);
-    hipLaunchKernelGGL(embed_combine_kernel, dim3((unsigned)nruns, (D + 255) / 256), dim3(256), 0, s, N, V, D, ksrc,
-                       partial, scale, dtable, accumulate);
+    if (N > 0) {
+        float *partial = reinterpret_cast<float *>(ws + w.partial);
+        const int nv = D / VEC<T>;
+        const long nruns = (N + RUN - 1) / RUN, tasks = nruns * ((nv + 63) / 64);
+        hipLaunchKernelGGL(embed_runs_kernel<T>, dim3((unsigned)(tasks < 4 * 65536 ? (tasks + 3) / 4 : 65536)), dim3(256), 0,
+                           s, N, V, nv, ksrc, psrc, dout, ldo, scale, dtable, accumulate, partial);
+        if (N > RUN)
+            hipLaunchKernelGGL(embed_combine_kernel, dim3((unsigned)(nruns < 16 * 16384 ? (nruns + 15) / 16 : 16384), (D + 255) / 256),
+                               dim3(1024), 0, s, N, V, D, ksrc, partial, scale, dtable, accumulate);
+    }
     return hipGetLastError();
 }
 

@@ -206,25 +206,59 @@ __global__ __launch_bounds__(THREADS<W>) void add_norm_backward_kernel(NormBwdAr
             store_vec<T>(dx + (long)c * E, o);
         }
     }
-    // one row of sums per wave group
+    // one row of sums per block: its waves' rows in order
     const long D = (long)nv * E;
-    float *out = a.partial + ((long)blockIdx.x * ROWS<W> + (W == 1 ? threadIdx.x >> 6 : 0)) * D;
+    if constexpr (W == 1) {
+        __shared__ float sums[ROWS<W>][64 * P * E];
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-        const int c = tid + p * 64 * W;
-        if (c >= nv) continue;
+        for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int e = 0; e < E; ++e) out[(long)c * E + e] = dg[p][e];
+            for (int e = 0; e < E; ++e) sums[threadIdx.x >> 6][(tid + p * 64) * E + e] = dg[p][e];
+        __syncthreads();
+        for (int c = threadIdx.x; c < D; c += THREADS<W>)
+            a.partial[blockIdx.x * D + c] = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
+    } else {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int c = tid + p * 64 * W;
+            if (c >= nv) continue;
+#pragma unroll
+            for (int e = 0; e < E; e += 4)
+                *reinterpret_cast<f32x4 *>(a.partial + blockIdx.x * D + (long)c * E + e) =
+                    f32x4{dg[p][e], dg[p][e + 1], dg[p][e + 2], dg[p][e + 3]};
+        }
     }
 }
 
-// Blocks of the backward pass: each leaves ROWS<W> rows of partial sums.
-constexpr int BWD_SLOTS = 1024;   // rows of partial sums at most
+// dg (+)= the sum of the blocks' rows: 32 groups of 16 lanes take every 32nd
+// row of 64 columns, and their sums are added in order.
+__global__ __launch_bounds__(512) void norm_gain_kernel(const float *__restrict__ partial, int rows, int D,
+                                                        float *__restrict__ dg, int accumulate)
+{
+    __shared__ f32x4 part[32][16];
+    const int lane = threadIdx.x & 15, grp = threadIdx.x >> 4, c = (blockIdx.x * 16 + lane) * 4;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    if (c < D)
+#pragma unroll 8
+        for (int r = grp; r < rows; r += 32) acc += *reinterpret_cast<const f32x4 *>(partial + (long)r * D + c);
+    part[grp][lane] = acc;
+    __syncthreads();
+    if (grp == 0 && c < D) {
+        f32x4 *p = reinterpret_cast<f32x4 *>(dg + c);
+        acc = accumulate ? *p : f32x4{0.f, 0.f, 0.f, 0.f};
+        f32x4 sum = part[0][lane];
+        for (int k = 1; k < 32; ++k) sum += part[k][lane];
+        *p = accumulate ? acc + sum : sum;
+    }
+}
+
+// Blocks of the backward pass, each of which leaves one row of partial sums.
+constexpr int BWD_BLOCKS = 512;
 
 int bwd_blocks(long rows, int rows_per_block)
 {
-    const long need = (rows + rows_per_block - 1) / rows_per_block, most = BWD_SLOTS / rows_per_block;
-    return (int)(need < most ? need : most);
+    const long need = (rows + rows_per_block - 1) / rows_per_block;
+    return (int)(need < BWD_BLOCKS ? need : BWD_BLOCKS);
 }
 
 template <typename T, int W, int P>
@@ -247,7 +281,9 @@ hipError_t launch_norm_bwd(const NormBwdArgs &a, hipStream_t s)
     hipLaunchKernelGGL((add_norm_backward_kernel<T, W, P>), dim3(blocks), dim3(THREADS<W>), 0, s, a, a.D / VEC<T>);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    return sum_rows(a.partial, blocks * ROWS<W>, a.D, a.dg, a.accumulate, s);
+    hipLaunchKernelGGL(norm_gain_kernel, dim3((a.D + 63) / 64), dim3(512), 0, s, a.partial, blocks, a.D, a.dg,
+                       a.accumulate);
+    return hipGetLastError();
 }
 
 // Waves and vectors per thread of a row of nv vectors.
@@ -288,13 +324,13 @@ hipError_t add_norm(DType t, const NormArgs &a, hipStream_t s)
     return t == DType::BF16 ? add_norm_t<bf16_t>(a, s) : add_norm_t<float>(a, s);
 }
 
-size_t norm_partial_floats(long rows, int D) { return (size_t)(rows < BWD_SLOTS ? rows + 3 : BWD_SLOTS) * D; }
+size_t norm_partial_floats(long rows, int D) { return (size_t)(rows < BWD_BLOCKS ? rows : BWD_BLOCKS) * D; }
 
 hipError_t add_norm_backward(DType t, const NormBwdArgs &a, hipStream_t s)
 {
     const double n = (double)a.rows * a.D;
-    ProfScope ps(K_NORM, s, 0.0, n * dsize(t) * (a.dsum ? 4.0 : 3.0));
     if (a.rows == 0) return a.accumulate ? hipSuccess : fill_u32(a.dg, a.D, 0u, s);
+    ProfScope ps(K_NORM, s, 0.0, n * dsize(t) * (a.dsum ? 4.0 : 3.0));
     return t == DType::BF16 ? add_norm_backward_t<bf16_t>(a, s) : add_norm_backward_t<float>(a, s);
 }
 

@@ -377,9 +377,11 @@ __global__ __launch_bounds__(256) void embed_runs_kernel(long N, long V, int nv,
     }
 }
 
-// Rows of more than RUN tokens: a block looks at 16 runs, one per wave, and its
-// waves add the partial sums of every long row that starts in one of them and
-// reaches over its end, a sixteenth each.
+// Rows of more than RUN tokens: a block looks at 16 runs, one per wave, for a
+// long row that starts in the run and reaches over its end.  The wave adds up
+// to ALONE partial sums by itself; of a longer row all the block's waves add a
+// sixteenth each.
+constexpr int ALONE = 32;
 __global__ __launch_bounds__(1024) void embed_combine_kernel(long N, long V, int D, const unsigned *__restrict__ keys,
                                                              const float *__restrict__ partial, float scale,
                                                              float *__restrict__ dtable, int accumulate)
@@ -397,16 +399,33 @@ __global__ __launch_bounds__(1024) void embed_combine_kernel(long N, long V, int
             const int last = 63 - __builtin_clzll((w.change | 1) & ((1ull << 2 * RUN) - 1));
             const unsigned key = __builtin_amdgcn_readlane(w.key, 2 * RUN - 1);
             if (key < (unsigned)V && last >= RUN && !(w.change >> 2 * RUN & 1) && next_change(w, 2 * RUN) - last > RUN) {
-                // the last run that starts with the row: 64 probes at a time
-                long lo = mine + 1, left = nruns - lo;   // run lo starts with it, run lo + left does not
+                long lo = mine + 1;
+                // the last run that starts with the row: among the next 64, or
+                // by 64 probes at a time
+                auto starting = [&](long step, long below) {   // of runs lo, lo + step, ...
+                    const long at = lo + lane * step;
+                    return __popcll(__ballot(at < below && keys[min(at, nruns - 1) * RUN] == key));
+                };
+                const int hits = starting(1, nruns);
+                lo += hits - 1;
+                long left = hits < 64 ? 1 : nruns - lo;   // run lo starts with it, run lo + left does not
                 while (left > 1) {
                     const long step = (left + 63) / 64;
-                    const long at = lo + lane * step;
-                    const int hits = __popcll(__ballot(at < lo + left && keys[min(at, nruns - 1) * RUN] == key));
-                    lo += (hits - 1) * step;
+                    lo += (starting(step, lo + left) - 1) * step;
                     left = min(step, nruns - lo);
                 }
                 runs = lo - mine + 1;
+                if (runs <= ALONE) {
+                    if (c < D) {
+                        f32x4 acc = *reinterpret_cast<const f32x4 *>(partial + (2 * mine + 1) * D + c);
+#pragma unroll 8
+                        for (long j = 1; j < runs; ++j)
+                            acc += *reinterpret_cast<const f32x4 *>(partial + 2 * (mine + j) * D + c);
+                        f32x4 *p = reinterpret_cast<f32x4 *>(dtable + (long)key * D + c);
+                        *p = accumulate ? *p + scale * acc : scale * acc;
+                    }
+                    runs = 0;
+                }
             }
         }
         if (lane == 0) owner_runs[wave] = runs;

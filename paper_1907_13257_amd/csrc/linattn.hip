@@ -28,7 +28,7 @@ struct Role {
     const float *X0;         // state before the first token; element (i, j) at i * si + j * sj of a head's K*M values
     float *XT;
     int si, sj;
-    float *parts;            // states of the parts [B*N][parts][da][dc], where the sequences are split
+    float *slots;            // where the sequences are split: states [B*N][parts], laid out as X0 (see below)
 };
 constexpr int MAX_ROLES = 3;
 template <typename T>
@@ -38,6 +38,8 @@ struct Roles {
     const int32_t *lengths;
     int T_, B, N;
     int parts, part_len;     // parts of a sequence, their tokens (a multiple of the chunk)
+    int tiles;               // result tiles of 16 columns per wave, 1 or 2
+    bool joined;             // the slots hold the states at the parts' starts
 };
 
 // decay^n; 0^0 = 1.  `lg` is log2(decay) rounded from 64 bits: log2 of a decay
@@ -54,8 +56,8 @@ __device__ __forceinline__ int sequence_length(const int32_t *lengths, int b, in
 
 // ---------------------------------------------------------------------------
 // Sequences, one chunk of C tokens after another.  A block has one head of one
-// batch row (or a part of its tokens); each of its waves owns 32 columns of
-// the state, which stay in its registers, and takes the chunk's rows of A and
+// batch row (or a part of its tokens); each of its waves owns 32 or 16 columns
+// of the state, which stay in its registers, and takes the chunk's rows of A and
 // B (shared) and C (its own columns) from LDS:
 //   out^T = decay^t X^T A^T + C^T P ,  P = (B A^T) * decay^(t-s) for s <= t
 //   X     = decay^C X + B^T (C decay^(C-1-s))
@@ -83,9 +85,6 @@ template <> struct Mat<float> {
     static constexpr int C = 16;
     static constexpr int TT = 1;
 };
-constexpr int MT = 2;              // result tiles of 16 columns per wave
-constexpr int WCOLS = 16 * MT;
-
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4_t;
@@ -116,45 +115,66 @@ template <int CH>
 struct Tile {
     static constexpr int PITCH = 1024 + 64;
     static constexpr int RPI = 64 / CH;    // rows of an instruction
-    __device__ static constexpr int flip(int row) { return ((row >> 2) & 1) * 2 + ((row >> 3) & 1); }
+    __device__ static constexpr int flip(int row) { return CH == 2 ? 0 : ((row >> 2) & 1) * 2 + ((row >> 3) & 1); }
     // instruction of a row, and its place there
     __device__ static constexpr int instr(int row)
     {
         const int hi = row >> 4;
-        return CH == 64 ? row : CH == 32 ? (row & 7) + 8 * hi : CH == 16 ? (row & 3) + 4 * hi : CH == 8 ? (row & 1) + 2 * hi : hi;
+        return CH == 64 ? row : CH == 32 ? (row & 7) + 8 * hi : CH == 16 ? (row & 3) + 4 * hi : CH == 8 ? (row & 1) + 2 * hi
+                                                                                            : CH == 4 ? hi : 0;
     }
     __device__ static constexpr int place(int row)
     {
         const int b1 = (row >> 1) & 1, b3 = (row >> 3) & 1;
         return CH == 64 ? 0 : CH == 32 ? b3 : CH == 16 ? flip(row) : CH == 8 ? b1 + 2 * b3 + 4 * ((row >> 2) & 1)
-                                                                             : (row & 3) + 4 * flip(row);
+                                                                             : CH == 4 ? (row & 3) + 4 * flip(row) : row;
     }
     __device__ static constexpr int offset(int row) { return instr(row) * PITCH + place(row) * CH * 16; }
     // the row of place j of instruction k: row_k(k) + row_j(j)
     __device__ static constexpr int row_k(int k)
     {
         return CH == 64 ? k : CH == 32 ? (k & 7) + 16 * (k >> 3) : CH == 16 ? (k & 3) + 16 * (k >> 2)
-                                                                   : CH == 8 ? (k & 1) + 16 * (k >> 1) : 16 * k;
+                                                                   : CH == 8 ? (k & 1) + 16 * (k >> 1) : CH == 4 ? 16 * k : 32 * k;
     }
     __device__ static constexpr int row_j(int j)
     {
         return CH == 64 ? 0 : CH == 32 ? 8 * j : CH == 16 ? 4 * (j >> 1) + 8 * (j & 1)
                                        : CH == 8 ? 2 * (j & 1) + 8 * ((j >> 1) & 1) + 4 * (j >> 2)
-                                                 : (j & 3) + 4 * ((j >> 3) & 1) + 8 * ((j >> 2) & 1);
+                                                 : CH == 4 ? (j & 3) + 4 * ((j >> 3) & 1) + 8 * ((j >> 2) & 1) : j;
     }
 };
 
-// Instruction k of a tile: rows of `width` elements, `step` apart, `rows` of
-// them; zeros elsewhere.
+// Where a lane's share of a tile's rows comes from: rows of `width` elements,
+// `step` apart.
 template <typename T, int CH>
-__device__ __forceinline__ void load_rows(const T *base, long step, int rows, int width, int k, unsigned tile, int lane)
-{
-    constexpr int E = 16 / (int)sizeof(T);
-    const int row = Tile<CH>::row_k(k) + Tile<CH>::row_j(lane / CH), c = (lane % CH) ^ Tile<CH>::flip(row);
-    const bool in = row < rows && c * E < width;
-    const void *p = in ? static_cast<const void *>(base + row * step + c * E) : static_cast<const void *>(zero_chunk);
-    dma16_from(p, __builtin_amdgcn_readfirstlane(tile + (unsigned)(k * Tile<CH>::PITCH)));
-}
+struct Loader {
+    static constexpr int E = 16 / (int)sizeof(T);
+    const T *own;   // the lane's row and chunk of instruction 0
+    long step;
+    int row, chunk, chunks;
+    __device__ __forceinline__ void init(const T *base, long step_, int width, int lane)
+    {
+        step = step_;
+        row = Tile<CH>::row_j(lane / CH);
+        chunk = (lane % CH) ^ Tile<CH>::flip(row);
+        chunks = width / E;
+        own = base + row * step + chunk * E;
+    }
+    // instruction k of the tile whose first row is token t0, `rows` of them; zeros
+    // elsewhere (`whole`: nowhere)
+    __device__ __forceinline__ void issue(int t0, int rows, int k, unsigned tile, bool whole) const
+    {
+        const int rk = Tile<CH>::row_k(k);
+        int c = chunk;
+        const T *p = own + (t0 + rk) * step;
+        if constexpr (CH >= 32) {   // such rows' bit 2 (and 3) is the instruction's
+            c ^= Tile<CH>::flip(rk);
+            p += (c - chunk) * E;
+        }
+        if (!whole && !(row + rk < rows && c < chunks)) p = reinterpret_cast<const T *>(zero_chunk);
+        dma16_from(p, __builtin_amdgcn_readfirstlane(tile + (unsigned)(k * Tile<CH>::PITCH)));
+    }
+};
 
 // Where a lane finds the operands of a tile.
 template <int CH, typename T> struct Reader;
@@ -211,29 +231,44 @@ struct Reader<CH, float> {
     }
 };
 
-__device__ __forceinline__ unsigned pack_bf16(float a, float b)
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ unsigned pack_bf16(float a, float b)   // one conversion instruction for both
 {
-    return (unsigned)f32_to_bf16(a) | ((unsigned)f32_to_bf16(b) << 16);
+    return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2{a, b}), bf16x2));
+}
+
+// What eight values leave over their packed bf16 parts w: x - bf16(x), one
+// instruction each, the dot product of a pair with (-1, 0) or (0, -1) added to
+// x (exact).  Written out because the compiler takes the form that overwrites x
+// and copies x first (94 copies per chunk).  A dot product's result may be read
+// three wait states later, which the block ends with; x may be a matrix
+// product's result, whose wait lies before w, made from x by an instruction the
+// compiler knows.
+__device__ __forceinline__ void left_over(const u32x4 w, const float (&x)[8], float (&r)[8])
+{
+    asm("v_dot2_f32_bf16 %0, %8, %20, %12\n\tv_dot2_f32_bf16 %1, %8, %21, %13\n\t"
+        "v_dot2_f32_bf16 %2, %9, %20, %14\n\tv_dot2_f32_bf16 %3, %9, %21, %15\n\t"
+        "v_dot2_f32_bf16 %4, %10, %20, %16\n\tv_dot2_f32_bf16 %5, %10, %21, %17\n\t"
+        "v_dot2_f32_bf16 %6, %11, %20, %18\n\tv_dot2_f32_bf16 %7, %11, %21, %19\n\ts_nop 2"
+        : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+        : "v"(w[0]), "v"(w[1]), "v"(w[2]), "v"(w[3]), "v"(x[0]), "v"(x[1]), "v"(x[2]), "v"(x[3]), "v"(x[4]), "v"(x[5]),
+          "v"(x[6]), "v"(x[7]), "s"(0x0000bf80u), "s"(0xbf800000u));
 }
 
 // fp32 values of an operand as the parts the matrix cores take.
 template <int NP>
 __device__ __forceinline__ void split(const float (&x)[8], u32x4 (&f)[NP], bf16_t)
 {
-    float r[8];
+    float r[NP][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = x[e];
+    for (int e = 0; e < 8; ++e) r[0][e] = x[e];
 #pragma unroll
-    for (int p = 0; p < NP; ++p)
+    for (int p = 0; p < NP; ++p) {
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-            const unsigned w = pack_bf16(r[e], r[e + 1]);
-            f[p][e / 2] = w;
-            if (p + 1 < NP) {
-                r[e] -= __uint_as_float(w << 16);
-                r[e + 1] -= __uint_as_float(w & 0xffff0000u);
-            }
-        }
+        for (int e = 0; e < 8; e += 2) f[p][e / 2] = pack_bf16(r[p][e], r[p][e + 1]);
+        if (p + 1 < NP) left_over(f[p], r[p], r[p + 1]);
+    }
 }
 template <int NP>
 __device__ __forceinline__ void split(const float (&x)[4], u32x4 (&f)[NP], float)
@@ -243,20 +278,37 @@ __device__ __forceinline__ void split(const float (&x)[4], u32x4 (&f)[NP], float
 
 // Four consecutive values of an output row.
 template <typename T> struct Out4;
-template <> struct Out4<bf16_t> { u32x2 v; };
-template <> struct Out4<float> { f32x4 v; };
-__device__ __forceinline__ Out4<bf16_t> out4(f32x4 a, bf16_t) { return {u32x2{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])}}; }
-__device__ __forceinline__ Out4<float> out4(f32x4 a, float) { return {a}; }
+template <> struct Out4<bf16_t> { typedef u32x2 type; };
+template <> struct Out4<float> { typedef f32x4 type; };
+__device__ __forceinline__ u32x2 out4(f32x4 a, bf16_t) { return u32x2{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])}; }
+__device__ __forceinline__ f32x4 out4(f32x4 a, float) { return a; }
 
-// OUT: rows of the output, from the state at the start of the part (and the
-// final state where nothing is split); else the state a part adds, from zero.
-// NP: parts of the state's update (bf16).
-template <typename T, int DA, bool OUT, int NP>
-__global__ __launch_bounds__(512) void linattn_chunks_kernel(Roles<T> g)
+// Chunks of 16 bytes a tile's row has in LDS: a power of two.
+template <typename T, int DA>
+constexpr int row_chunks()
+{
+    int c = 4;
+    while (c * 16 < DA * (int)sizeof(T)) c *= 2;
+    return c;
+}
+
+// A long sequence of few heads is split into parts: a first launch (not OUT)
+// leaves in slot p + 1 the state that the tokens of part p add, and in slot 0
+// the first state (which the final one may replace while other blocks run); the
+// second (OUT) starts a part from slots 0 .. p, joined with the decays between
+// them, by itself or, where they are many, from what linattn_join_kernel made of
+// them.  The last part of a sequence adds to no other and has no slot.
+//
+// OUT: rows of the output, and the final state; else the slots.
+// NP: parts of the state's update (bf16).  DA: the width of A and B, padded
+// with zeros to a multiple of 32.  MT: result tiles of 16 columns per wave.
+template <typename T, int DA, bool OUT, int NP, int MT>
+__global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(Roles<T> g)
 {
     constexpr int C = Mat<T>::C, TT = Mat<T>::TT, E = C / 4;   // E: values of an operand per lane
-    constexpr int CHA = DA * (int)sizeof(T) / 16, CHC = WCOLS * (int)sizeof(T) / 16;
-    constexpr int KB = DA / C, KT = DA / 16;
+    constexpr int WCOLS = 16 * MT;                             // columns of a wave
+    constexpr int CHA = row_chunks<T, DA>(), CHC = WCOLS * (int)sizeof(T) / 16;
+    constexpr int KB = DA / C, KT = DA / 16, KEEP = KB < 4 ? KB : 4;
     constexpr int NA = C * CHA / 64, NC = C * CHC / 64;        // load instructions of a tile
     constexpr int ABYTES = NA * Tile<CHA>::PITCH, CBYTES = NC * Tile<CHC>::PITCH;
     constexpr int SP = sizeof(T) == 2 ? 2 : 1;                 // parts of X and P
@@ -266,56 +318,91 @@ __global__ __launch_bounds__(512) void linattn_chunks_kernel(Roles<T> g)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = blockIdx.x % g.N, b = (int)((blockIdx.x / g.N) % g.B), part = (int)(blockIdx.x / g.N / g.B);
     const long bh = (long)b * g.N + h;
-    const int n = sequence_length(g.lengths, b, g.T_);
+    // (a value read from memory that is the same for all lanes stays in a scalar
+    // register only if it is said to be)
+    const int n = __builtin_amdgcn_readfirstlane(sequence_length(g.lengths, b, g.T_));
     const int begin = part * g.part_len, stop = min(g.T_, begin + g.part_len), end = min(n, stop);
     const int da = r.da, dc = r.dc, col0 = wave * WCOLS;
+    T *const out = r.out;
+    const long size = (long)da * dc, slots = bh * g.parts * size;
+    const bool last = end >= n;   // of this sequence
+    float *const XT = OUT && last && (n > 0 || part == 0) ? r.XT : nullptr;
 
-    if (OUT && !r.out && g.parts > 1) return;   // the final state is known
-    if (OUT && r.out)   // behind the sequence's end
-        for (int t = max(n, begin); t < stop; ++t)
-            for (int c = threadIdx.x; c < dc; c += blockDim.x)
-                r.out[((long)t * g.B + b) * r.ldo + (long)h * dc + c] = from_f32<T>(0.0f);
+    if (!OUT && part == 0 && r.X0)   // the first state
+        for (int i = threadIdx.x; i < size / 4; i += blockDim.x)
+            reinterpret_cast<f32x4 *>(r.slots + slots)[i] = reinterpret_cast<const f32x4 *>(r.X0 + bh * size)[i];
+    if (!OUT && last) return;
+    if (OUT && !out && !XT) return;
+    if (OUT && out && n < stop) {   // behind the sequence's end
+        const int per = dc * (int)sizeof(T) / 16, t0 = max(n, begin), all = (stop - t0) * per;
+        for (int i = threadIdx.x; i < all; i += blockDim.x) {
+            T *row = out + ((long)(t0 + i / per) * g.B + b) * r.ldo + (long)h * dc;
+            reinterpret_cast<u32x4 *>(row)[i % per] = zero16();
+        }
+    }
     if (begin >= end && (part > 0 || !OUT)) return;
 
-    // rows of token i of the sequence: at + i * step
+    // rows of token i of the sequence: first + i * dir
     const long first = r.reverse ? (long)(n - 1) * g.B + b : b, dir = r.reverse ? -g.B : g.B;
-    const T *A = r.a + first * r.lda + (long)h * da, *Bp = r.b + first * r.ldb + (long)h * da;
-    const T *Cp = r.c + first * r.ldc + (long)h * dc + col0;
-    const long sa = dir * r.lda, sb = dir * r.ldb, sc = dir * r.ldc;
 
-    // LDS: two buffers of A, B and every wave's columns of C
-    const int buf_bytes = (OUT ? 2 : 1) * ABYTES + waves * CBYTES;
+    // LDS: two buffers of a chunk's rows of A and B and every wave's columns of C
+    const int chunk_bytes = (OUT ? 2 : 1) * ABYTES + waves * CBYTES;
     const unsigned lds0 = lds_addr(lds);
+    Loader<T, CHA> la, lb;
+    Loader<T, CHC> lc;
+    if (OUT) la.init(r.a + first * r.lda + (long)h * da, dir * r.lda, da, lane);
+    lb.init(r.b + first * r.ldb + (long)h * da, dir * r.ldb, da, lane);
+    lc.init(r.c + first * r.ldc + (long)h * dc + col0, dir * r.ldc, dc - col0, lane);
     auto issue = [&](int t0, int buf) {
-        const unsigned base = lds0 + (unsigned)(buf * buf_bytes);
         const int rows = min(C, end - t0);
-        for (int k = wave; k < NA; k += waves) {
-            load_rows<T, CHA>(Bp + t0 * sb, sb, rows, da, k, base, lane);
-            if (OUT) load_rows<T, CHA>(A + t0 * sa, sa, rows, da, k, base + ABYTES, lane);
+        const unsigned base = lds0 + (unsigned)(buf * chunk_bytes);
+        if (rows == C && da * (int)sizeof(T) == CHA * 16) {
+#pragma unroll 1
+            for (int k = wave; k < NA; k += waves) {
+                lb.issue(t0, C, k, base, true);
+                if (OUT) la.issue(t0, C, k, base + ABYTES, true);
+            }
+        } else {
+#pragma unroll 1
+            for (int k = wave; k < NA; k += waves) {
+                lb.issue(t0, rows, k, base, false);
+                if (OUT) la.issue(t0, rows, k, base + ABYTES, false);
+            }
         }
 #pragma unroll
-        for (int k = 0; k < NC; ++k)
-            load_rows<T, CHC>(Cp + t0 * sc, sc, rows, dc - col0, k, base + (OUT ? 2 : 1) * ABYTES + wave * CBYTES, lane);
+        for (int k = 0; k < NC; ++k) lc.issue(t0, rows, k, base + (OUT ? 2 : 1) * ABYTES + wave * CBYTES, false);
     };
     if (begin < end) issue(begin, 0);
 
+    const float lg = decay_log2(g.decay[h]);
     // the state: element (16 kt + 4 q + v, col0 + 16 mt + c16) in X[kt][mt][v]
     f32x4 X[KT][MT];
-    const float *start = !OUT ? nullptr : g.parts > 1 ? r.parts + (bh * g.parts + part) * da * dc
-                                                      : (r.X0 ? r.X0 + bh * da * dc : nullptr);
-    const int si = g.parts > 1 ? dc : r.si, sj = g.parts > 1 ? 1 : r.sj;
+    const int si = r.si, sj = r.sj;
+    const int own = 4 * q * si + (col0 + c16) * sj;   // the lane's element (0, 0, 0)
+    bool zero = true;   // X is zero
+    auto join = [&](const float *from, float keep) {   // X = keep X + from
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            if (kt % 4 == 0) __builtin_amdgcn_sched_barrier(0);   // loads of four tiles in flight, not of all
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+                if (16 * kt + 4 * q < da && col0 + 16 * mt + c16 < dc)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        X[kt][mt][v] = from[own + (16 * kt + v) * si + 16 * mt * sj] + keep * X[kt][mt][v];
+        }
+        zero = false;
+    };
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int i = 16 * kt + 4 * q + v, j = col0 + 16 * mt + c16;
-                X[kt][mt][v] = start && i < da && j < dc ? start[i * si + j * sj] : 0.0f;
-            }
-    bool zero = !start;   // X is zero
+        for (int mt = 0; mt < MT; ++mt) X[kt][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (OUT) {
+        if (r.X0) join(g.parts > 1 ? r.slots + slots : r.X0 + bh * size, 0.0f);
+        const float keep = part > 0 && !g.joined ? decay_pow(lg, g.part_len) : 0.0f;
+        for (int k = g.joined ? max(part, 1) : 1; k <= part; ++k) join(r.slots + slots + k * size, keep);
+    }
 
-    const float lg = decay_log2(g.decay[h]);
     // decays between the state and the row of the first token: one forwards; the
     // state of the backward directions stands at that token, one decay further
     const int pre = r.reverse ? 0 : 1;
@@ -333,32 +420,24 @@ __global__ __launch_bounds__(512) void linattn_chunks_kernel(Roles<T> g)
     float wc[E];          // the tokens' factors in the chunk's final state
     int wc_rows = -1;     // for a chunk of so many tokens
     float whole = 1.0f;   // the state's factor over that chunk
+    // The state is gain * X: a chunk's decay goes into gain, its tokens are
+    // added divided by gain, and X is multiplied only when gain gets small
+    // (one chunk in many for the usual decays)
+    float gain = 1.0f;
 
     Reader<CHA, T> ra;
     Reader<CHC, T> rc;
     ra.init(c16, q);
     rc.init(c16, q);
-    Out4<T> held[TT][MT];   // the last chunk's output, stored while the next one is computed
-    auto store = [&](int t0) {
-        if (!r.out) return;
-#pragma unroll
-        for (int ti = 0; ti < TT; ++ti) {
-            const int t = t0 + 16 * ti + c16;
-            if (t >= end) continue;
-            T *row = r.out + (first + t * dir) * r.ldo + (long)h * dc + col0 + 4 * q;
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-                if (col0 + 16 * mt + 4 * q < dc) *reinterpret_cast<Out4<T> *>(row + 16 * mt) = held[ti][mt];
-        }
-    };
+    const long ldo = r.ldo, sto = dir * ldo;
+    T *orow = OUT && out ? out + (first + (begin + c16) * dir) * ldo + (long)h * dc + col0 + 4 * q : nullptr;
 
     int buf = 0;
     for (int t0 = begin; t0 < end; t0 += C, buf ^= 1) {
         waitcnt_vm<0>();   // this chunk's rows
         __syncthreads();   // everyone's; and the other buffer has been read
         if (t0 + C < end) issue(t0 + C, buf ^ 1);
-        if (OUT && t0 > begin) store(t0 - C);
-        lds_char *tb = (lds_char *)lds + buf * buf_bytes, *ta = tb + ABYTES;
+        lds_char *tb = (lds_char *)lds + buf * chunk_bytes, *ta = tb + ABYTES;
         lds_char *tc = tb + (OUT ? 2 : 1) * ABYTES + wave * CBYTES;
         const int rows = min(C, end - t0);
 
@@ -367,63 +446,95 @@ __global__ __launch_bounds__(512) void linattn_chunks_kernel(Roles<T> g)
         for (int mt = 0; mt < MT; ++mt) ct[mt] = rc.col(tc, mt);
 
         if constexpr (OUT) {
-            // X^T A^T, and P^T: tile of tokens s (rows) by tile of tokens ti (columns)
-            f32x4 o[TT][MT], P[TT][TT];
-#pragma unroll
-            for (int ti = 0; ti < TT; ++ti) {
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) o[ti][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int s = 0; s <= ti; ++s) P[s][ti] = f32x4{0.f, 0.f, 0.f, 0.f};
-            }
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                u32x4 a[TT];
-#pragma unroll
-                for (int ti = 0; ti < TT; ++ti) a[ti] = ra.row(ta, ti, kb);
-#pragma unroll
-                for (int s = 0; s < TT; ++s) {
-                    const u32x4 bf = ra.row(tb, s, kb);
-#pragma unroll
-                    for (int ti = s; ti < TT; ++ti) mfma16(P[s][ti], bf, a[ti], T());
-                }
-                if (!zero)
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        float x[E];
-#pragma unroll
-                        for (int e = 0; e < E; ++e) x[e] = X[TT * kb + e / 4][mt][e % 4];
-                        u32x4 f[SP];
-                        split<SP>(x, f, T());
-#pragma unroll
-                        for (int p = 0; p < SP; ++p)
-#pragma unroll
-                            for (int ti = 0; ti < TT; ++ti) mfma16(o[ti][mt], f[p], a[ti], T());
-                    }
-            }
+            // P^T: tile of tokens s (rows) by tile of tokens ti (columns)
+            f32x4 P[TT][TT];
 #pragma unroll
             for (int ti = 0; ti < TT; ++ti)
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) o[ti][mt] *= rowf[ti];
+                for (int s = 0; s <= ti; ++s) P[s][ti] = f32x4{0.f, 0.f, 0.f, 0.f};
+            // the operands of all column blocks are read before the first product
+            // waits for one (up to KEEP blocks: registers), and A's stay
+            u32x4 a[TT][KEEP], bf[TT][KEEP];
+            auto read = [&](int kb) {
+#pragma unroll
+                for (int ti = 0; ti < TT; ++ti) {
+                    a[ti][kb % KEEP] = ra.row(ta, ti, kb);
+                    bf[ti][kb % KEEP] = ra.row(tb, ti, kb);
+                }
+            };
+#pragma unroll
+            for (int k0 = 0; k0 < KB; k0 += KEEP) {
+#pragma unroll
+                for (int kb = k0; kb < k0 + KEEP && kb < KB; ++kb) read(kb);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int kb = k0; kb < k0 + KEEP && kb < KB; ++kb)
+#pragma unroll
+                    for (int s = 0; s < TT; ++s)
+#pragma unroll
+                        for (int ti = s; ti < TT; ++ti) mfma16(P[s][ti], bf[s][kb % KEEP], a[ti][kb % KEEP], T());
+            }
+            u32x4 pf[TT][SP];
 #pragma unroll
             for (int ti = 0; ti < TT; ++ti) {
                 float x[E];
 #pragma unroll
                 for (int e = 0; e < E; ++e)
                     x[e] = e / 4 > ti ? 0.0f : P[e / 4][ti][e % 4] * (e / 4 == ti ? w0[e % 4] : w1[e % 4]);
-                u32x4 f[SP];
-                split<SP>(x, f, T());
+                split<SP>(x, pf[ti], T());
+            }
+            // X^T A^T, scaled by row, and C^T P onto it
+            f32x4 o[TT][MT];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
+            for (int ti = 0; ti < TT; ++ti)
 #pragma unroll
-                    for (int p = 0; p < SP; ++p) mfma16(o[ti][mt], ct[mt], f[p], T());
-                    held[ti][mt] = out4(o[ti][mt], T());
+                for (int mt = 0; mt < MT; ++mt) o[ti][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (!zero) {
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) {
+                    if constexpr (KB > KEEP)
+#pragma unroll
+                        for (int ti = 0; ti < TT; ++ti) a[ti][kb % KEEP] = ra.row(ta, ti, kb);
+                    u32x4 f[MT][SP];
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        float x[E];
+#pragma unroll
+                        for (int e = 0; e < E; ++e) x[e] = X[TT * kb + e / 4][mt][e % 4];
+                        split<SP>(x, f[mt], T());
+                    }
+#pragma unroll
+                    for (int p = 0; p < SP; ++p)   // neighbours add to different tiles
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                            for (int ti = 0; ti < TT; ++ti) mfma16(o[ti][mt], f[mt][p], a[ti][kb % KEEP], T());
+                }
+#pragma unroll
+                for (int ti = 0; ti < TT; ++ti) {
+                    const float f = rowf[ti] * gain;
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) o[ti][mt] *= f;
                 }
             }
+#pragma unroll
+            for (int p = 0; p < SP; ++p)
+#pragma unroll
+                for (int ti = 0; ti < TT; ++ti)
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) mfma16(o[ti][mt], ct[mt], pf[ti][p], T());
+#pragma unroll
+            for (int ti = 0; ti < TT; ++ti)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    if (orow && 16 * ti + c16 < rows && col0 + 16 * mt + 4 * q < dc)
+                        *reinterpret_cast<typename Out4<T>::type *>(orow + 16 * ti * sto + 16 * mt) = out4(o[ti][mt], T());
+                }
+            if (orow) orow += C * sto;
         }
 
         // the state behind the chunk
-        if (!OUT || t0 + C < end || (g.parts == 1 && r.XT)) {
+        if (!OUT || t0 + C < end || XT) {
             if (rows != wc_rows) {
                 wc_rows = rows;
                 whole = decay_pow(lg, rows);
@@ -433,6 +544,18 @@ __global__ __launch_bounds__(512) void linattn_chunks_kernel(Roles<T> g)
                     wc[e] = left < 0 ? 0.0f : r.update * decay_pow(lg, left + 1 - pre);
                 }
             }
+            gain *= whole;
+            if (__builtin_amdgcn_readfirstlane(gain < 0x1p-20f)) {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) X[kt][mt] *= gain;
+                gain = 1.0f;
+            }
+            const float inv = 1.0f / gain;
+            float w[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) w[e] = wc[e] * inv;
             u32x4 f[MT][NP];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
@@ -440,135 +563,155 @@ __global__ __launch_bounds__(512) void linattn_chunks_kernel(Roles<T> g)
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     if constexpr (sizeof(T) == 2)
-                        x[e] = __uint_as_float(e % 2 ? ct[mt][e / 2] & 0xffff0000u : ct[mt][e / 2] << 16) * wc[e];
+                        x[e] = __uint_as_float(e % 2 ? ct[mt][e / 2] & 0xffff0000u : ct[mt][e / 2] << 16) * w[e];
                     else
-                        x[e] = __uint_as_float(ct[mt][e]) * wc[e];
+                        x[e] = __uint_as_float(ct[mt][e]) * w[e];
                 }
                 split<NP>(x, f[mt], T());
             }
+            constexpr int AHEAD = KT < 4 ? KT : 4;
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                const u32x4 bt = ra.col(tb, kt);
+            for (int k0 = 0; k0 < KT; k0 += AHEAD) {
+                u32x4 bt[AHEAD];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    X[kt][mt] *= whole;
+                for (int k = 0; k < AHEAD && k0 + k < KT; ++k) bt[k] = ra.col(tb, k0 + k);
 #pragma unroll
-                    for (int p = 0; p < NP; ++p) mfma16(X[kt][mt], bt, f[mt][p], T());
-                }
+                for (int p = 0; p < NP; ++p)
+#pragma unroll
+                    for (int k = 0; k < AHEAD && k0 + k < KT; ++k)
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) mfma16(X[k0 + k][mt], bt[k], f[mt][p], T());
             }
             zero = false;
         }
     }
-    if (OUT && begin < end) store(begin + (end - 1 - begin) / C * C);
 
-    // the part's state, or the sequence's final one
-    float *fin = !OUT ? r.parts + (bh * g.parts + part) * da * dc : (g.parts == 1 && r.XT ? r.XT + bh * da * dc : nullptr);
+    // what the part adds, or the sequence's final state
+    float *fin = !OUT ? r.slots + slots + (part + 1) * size : (XT ? XT + bh * size : nullptr);
     if (!fin) return;
-    const int fi = OUT ? r.si : dc, fj = OUT ? r.sj : 1;
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
+            if (16 * kt + 4 * q < da && col0 + 16 * mt + c16 < dc)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int i = 16 * kt + 4 * q + v, j = col0 + 16 * mt + c16;
-                if (i < da && j < dc) fin[i * fi + j * fj] = X[kt][mt][v];
-            }
+                for (int v = 0; v < 4; ++v) fin[own + (16 * kt + v) * si + 16 * mt * sj] = gain * X[kt][mt][v];
 }
 
-// The parts' states, in order: on entry what each part adds, on exit the state
-// at its start; and the final state.
+// Turns the slots into the states at the parts' starts.  A batch of them is read
+// before the first is written.
 template <typename T>
-__global__ __launch_bounds__(256) void linattn_scan_kernel(Roles<T> g)
+__global__ __launch_bounds__(256) void linattn_join_kernel(Roles<T> g)
 {
+    constexpr int BATCH = 8;
     const Role<T> &r = g.r[blockIdx.y];
-    const int per = (r.da * r.dc + 255) / 256;
+    const int size = r.da * r.dc, per = (size / 4 + 255) / 256;
     const long bh = blockIdx.x / per;
-    const int e = (int)(blockIdx.x % per) * 256 + threadIdx.x;
-    if (e >= r.da * r.dc) return;
+    const int e = ((int)(blockIdx.x % per) * 256 + threadIdx.x) * 4;
+    if (e >= size) return;
     const int n = sequence_length(g.lengths, (int)(bh / g.N), g.T_);
-    const float lg = decay_log2(g.decay[bh % g.N]);
-    const long at = bh * r.da * r.dc + (e / r.dc) * r.si + (e % r.dc) * r.sj;
-    float x = r.X0 ? r.X0[at] : 0.0f;
-    float *p = r.parts + bh * g.parts * (long)(r.da * r.dc) + e;
-    for (int k = 0; k < g.parts && k * g.part_len < n; ++k, p += r.da * r.dc) {
-        const float add = *p;
-        *p = x;
-        x = decay_pow(lg, min(g.part_len, n - k * g.part_len)) * x + add;
+    const int live = (n + g.part_len - 1) / g.part_len;   // slots 1 .. live - 1 are filled
+    f32x4 *p = reinterpret_cast<f32x4 *>(r.slots + bh * g.parts * (long)size + e);
+    f32x4 x = r.X0 ? *p : f32x4{0.f, 0.f, 0.f, 0.f};
+    const float keep = decay_pow(decay_log2(g.decay[bh % g.N]), g.part_len);
+    for (int k0 = 1; k0 < live; k0 += BATCH) {
+        f32x4 add[BATCH];
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k)
+            if (k0 + k < live) add[k] = p[(long)(k0 + k) * (size / 4)];
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k)
+            if (k0 + k < live) p[(long)(k0 + k) * (size / 4)] = x = keep * x + add[k];
     }
-    if (r.XT) r.XT[at] = x;
 }
 
 struct SplitPlan {
-    int parts, len;
+    int parts, len, tiles;
 };
 
-// Parts a sequence is split into: as many as it takes to give the chip
-// TARGET_WAVES waves, but none shorter than MIN_CHUNKS chunks.
-constexpr int TARGET_WAVES = 2048, MIN_CHUNKS = 4;
-SplitPlan split_plan(const LinAttnShape &sh, int chunk, int roles, int dc)
+// How a call is spread over the chip's 1024 SIMDs.  Sequences are split into as
+// many parts as it takes to give the chip TARGET_WAVES waves of 32 columns, but
+// none shorter than MIN_CHUNKS chunks.  A wave has 32 columns: P and the shared
+// rows cost a wave the same for 16.  Where that leaves the SIMDs with less than
+// one wave each unsplit and few chunks in all (FEW_CHUNKS of a wave per SIMD),
+// time is the latency of a wave's chunks, and 16 columns halve it: 2 x 1999
+// tokens of 16 heads of 64 in 36 us with 32 columns and 29 with 16, 12 x 333 of
+// 5 heads in fp32, forward and backward, 90 and 75; but 128 x 50 tokens of 16
+// heads 52 and 67, 4 x 4096 of 16 heads of 128 467 and 526.
+constexpr int TARGET_WAVES = 2048, MIN_CHUNKS = 3, FEW_CHUNKS = 16, SIMDS = 1024;
+SplitPlan split_plan(const LinAttnShape &sh, int chunk, int roles)
 {
-    const long waves = (long)sh.B * sh.N * roles * ((dc + WCOLS - 1) / WCOLS);
+    const int width = sh.K > sh.M ? sh.K : sh.M;
+    const long waves = (long)sh.B * sh.N * roles * ((width + 31) / 32);
     const int chunks = (sh.T + chunk - 1) / chunk;
     long parts = (TARGET_WAVES + waves - 1) / waves;
     const long most = chunks / MIN_CHUNKS;
     if (parts > most) parts = most;
     if (parts < 1) parts = 1;
     const int per = (int)((chunks + parts - 1) / parts);
-    return SplitPlan{(chunks + per - 1) / per, per * chunk};
+    const bool few = waves < SIMDS && waves * chunks < (long)FEW_CHUNKS * SIMDS && width <= 128;
+    return SplitPlan{(chunks + per - 1) / per, per * chunk, few ? 1 : 2};
 }
 
-template <typename T, int DA, bool OUT, int NP>
-hipError_t launch_chunks(const Roles<T> &g, int roles, hipStream_t s)
+template <typename T, int DA, bool OUT, int NP, int MT>
+hipError_t launch_chunks(const Roles<T> &g, int roles, int width, hipStream_t s)
 {
-    constexpr int C = Mat<T>::C;
-    const int waves = (g.r[0].dc + WCOLS - 1) / WCOLS;
-    constexpr int CHA = DA * (int)sizeof(T) / 16, CHC = WCOLS * (int)sizeof(T) / 16;
+    constexpr int WCOLS = 16 * MT;
+    constexpr int C = Mat<T>::C, CHA = row_chunks<T, DA>(), CHC = WCOLS * (int)sizeof(T) / 16;
+    const int waves = (width + WCOLS - 1) / WCOLS;
     const int lds = 2 * (C * CHA / 64 * (OUT ? 2 : 1) * Tile<CHA>::PITCH + C * CHC / 64 * waves * Tile<CHC>::PITCH);
     if (lds > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(linattn_chunks_kernel<T, DA, OUT, NP>),
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(linattn_chunks_kernel<T, DA, OUT, NP, MT>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((linattn_chunks_kernel<T, DA, OUT, NP>), dim3((unsigned)((long)g.B * g.N * g.parts), roles),
+    hipLaunchKernelGGL((linattn_chunks_kernel<T, DA, OUT, NP, MT>), dim3((unsigned)((long)g.B * g.N * g.parts), roles),
                        dim3(64 * waves), lds, s, g);
     return hipGetLastError();
 }
 
+// Roles of one launch: padded to the widest of them.
 template <typename T, bool OUT, int NP>
 hipError_t launch_width(const Roles<T> &g, int roles, hipStream_t s)
 {
-    const int da = g.r[0].da;
-    if (da <= 32) return launch_chunks<T, 32, OUT, NP>(g, roles, s);
-    if (da <= 64) return launch_chunks<T, 64, OUT, NP>(g, roles, s);
-    if (da <= 128) return launch_chunks<T, 128, OUT, NP>(g, roles, s);
-    return launch_chunks<T, 256, OUT, NP>(g, roles, s);
+    int da = 0, dc = 0;
+    for (int k = 0; k < roles; ++k) {
+        da = g.r[k].da > da ? g.r[k].da : da;
+        dc = g.r[k].dc > dc ? g.r[k].dc : dc;
+    }
+    const bool one = g.tiles == 1;
+    switch ((da + 31) / 32) {
+    case 1: return one ? launch_chunks<T, 32, OUT, NP, 1>(g, roles, dc, s) : launch_chunks<T, 32, OUT, NP, 2>(g, roles, dc, s);
+    case 2: return one ? launch_chunks<T, 64, OUT, NP, 1>(g, roles, dc, s) : launch_chunks<T, 64, OUT, NP, 2>(g, roles, dc, s);
+    case 3: return one ? launch_chunks<T, 96, OUT, NP, 1>(g, roles, dc, s) : launch_chunks<T, 96, OUT, NP, 2>(g, roles, dc, s);
+    case 4: return one ? launch_chunks<T, 128, OUT, NP, 1>(g, roles, dc, s) : launch_chunks<T, 128, OUT, NP, 2>(g, roles, dc, s);
+    case 5: return launch_chunks<T, 160, OUT, NP, 2>(g, roles, dc, s);
+    case 6: return launch_chunks<T, 192, OUT, NP, 2>(g, roles, dc, s);
+    case 7: return launch_chunks<T, 224, OUT, NP, 2>(g, roles, dc, s);
+    default: return launch_chunks<T, 256, OUT, NP, 2>(g, roles, dc, s);
+    }
 }
 
-// Roles of equal widths, at once; `planned` of them if all were wanted (results
-// do not depend on which are).  `states`: the call carries states, so that one
-// may be an output.  `parts`: workspace of all roles.
+// Parts from which on their states are joined by a launch of its own.  A block's
+// own joins cost it about 1.5 us each, the launch 8 us.
+constexpr int JOIN_PARTS = 6;
 template <typename T>
-hipError_t launch_roles(Roles<T> &g, int roles, int planned, bool states, const LinAttnShape &sh, float *parts, hipStream_t s)
+hipError_t launch_join(const Roles<T> &g, int roles, hipStream_t s)
 {
-    const SplitPlan p = split_plan(sh, Mat<T>::C, planned, g.r[0].dc);
-    g.T_ = sh.T; g.B = sh.B; g.N = sh.N;
-    g.parts = p.parts;
-    g.part_len = p.len;
-    for (int k = 0; k < roles; ++k)
-        g.r[k].parts = parts + (size_t)k * sh.B * sh.N * p.parts * sh.K * sh.M;
-    constexpr int MORE = sizeof(T) == 2 ? 3 : 1, FEWER = sizeof(T) == 2 ? 2 : 1;
-    hipError_t e;
-    if (p.parts > 1) {
-        e = states ? launch_width<T, false, MORE>(g, roles, s) : launch_width<T, false, FEWER>(g, roles, s);
-        if (e != hipSuccess) return e;
-        const int per = (sh.K * sh.M + 255) / 256;
-        hipLaunchKernelGGL(linattn_scan_kernel<T>, dim3((unsigned)((long)sh.B * sh.N * per), roles), dim3(256), 0, s, g);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        states = false;
-    }
-    return states ? launch_width<T, true, MORE>(g, roles, s) : launch_width<T, true, FEWER>(g, roles, s);
+    const int per = (g.r[0].da * g.r[0].dc / 4 + 255) / 256;
+    hipLaunchKernelGGL(linattn_join_kernel<T>, dim3((unsigned)((long)g.B * g.N * per), roles), dim3(256), 0, s, g);
+    return hipGetLastError();
+}
+
+// `exact`: the call carries states, so that one may be an output: three bf16
+// parts, whichever results are wanted (the rows do not depend on that).
+template <typename T, bool OUT>
+hipError_t launch_roles(const Roles<T> &g, int roles, bool exact, hipStream_t s)
+{
+    if constexpr (sizeof(T) == 2)
+        return exact ? launch_width<T, OUT, 3>(g, roles, s) : launch_width<T, OUT, 2>(g, roles, s);
+    else
+        return launch_width<T, OUT, 1>(g, roles, s);
 }
 
 // One token of one head per block: the state's rows are read four values per
@@ -616,15 +759,34 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(int B, int N, int K, 
 }
 
 template <typename T>
+Roles<T> call_of(const LinAttnShape &sh, const float *decay, const int32_t *lengths, int roles)
+{
+    Roles<T> g{};
+    const SplitPlan p = split_plan(sh, Mat<T>::C, roles);
+    g.decay = decay;
+    g.lengths = lengths;
+    g.T_ = sh.T; g.B = sh.B; g.N = sh.N;
+    g.parts = p.parts;
+    g.part_len = p.len;
+    g.tiles = p.tiles;
+    g.joined = p.parts >= JOIN_PARTS;
+    return g;
+}
+
+template <typename T>
 hipError_t forward_t(const LinAttnShape &sh, const T *q, const T *k, const T *v, const float *decay,
                      const int32_t *lengths, const float *S0, T *o, float *ST, float *ws, hipStream_t s)
 {
-    Roles<T> g{};
-    g.decay = decay;
-    g.lengths = lengths;
+    Roles<T> g = call_of<T>(sh, decay, lengths, 1);
     g.r[0] = Role<T>{q, k, v, o, sh.ldq, sh.ldk, sh.ldv, sh.ldo, sh.K, sh.M, false, sh.scale, sh.scale, 1.0f, S0, ST,
-                     sh.M, 1, nullptr};
-    return launch_roles(g, 1, 1, S0 || ST, sh, ws, s);
+                     sh.M, 1, ws};
+    const bool exact = S0 || ST;
+    if (g.parts > 1) {
+        hipError_t e = launch_roles<T, false>(g, 1, exact, s);
+        if (e == hipSuccess && g.joined) e = launch_join(g, 1, s);
+        if (e != hipSuccess) return e;
+    }
+    return launch_roles<T, true>(g, 1, exact, s);
 }
 
 template <typename T>
@@ -634,26 +796,31 @@ hipError_t backward_t(const LinAttnShape &sh, const T *d_o, const T *q, const T 
 {
     const int K = sh.K, M = sh.M;
     const float sc = sh.scale;
-    const bool states = S0 || dST || dS0;
-    const Role<T> rq{d_o, v, k, dq, sh.ldo, sh.ldv, sh.ldk, sh.ldq, M, K, false, sc, sc, 1.0f, S0, nullptr, 1, M, nullptr};
-    const Role<T> rk{v, d_o, q, dk, sh.ldv, sh.ldo, sh.ldq, sh.ldk, M, K, true, sc, 1.0f, sc, dST, nullptr, 1, M, nullptr};
-    const Role<T> rv{k, q, d_o, dv, sh.ldk, sh.ldq, sh.ldo, sh.ldv, K, M, true, sc, 1.0f, sc, dST, dS0, M, 1, nullptr};
-    Roles<T> g{};
-    g.decay = decay;
-    g.lengths = lengths;
+    Roles<T> g = call_of<T>(sh, decay, lengths, MAX_ROLES);
+    // the states of dk and dv are each other's transposes: dv's slots serve both
+    float *const ws2 = ws + (g.parts > 1 ? (size_t)sh.B * sh.N * g.parts * K * M : 0);
+    const Role<T> rq{d_o, v, k, dq, sh.ldo, sh.ldv, sh.ldk, sh.ldq, M, K, false, sc, sc, 1.0f, S0, nullptr, 1, M, ws};
+    const Role<T> rk{v, d_o, q, dk, sh.ldv, sh.ldo, sh.ldq, sh.ldk, M, K, true, sc, 1.0f, sc, dST, nullptr, 1, M, ws2};
+    const Role<T> rv{k, q, d_o, dv, sh.ldk, sh.ldq, sh.ldo, sh.ldv, K, M, true, sc, 1.0f, sc, dST, dS0, M, 1, ws2};
+    const bool exact = S0 || dST || dS0, back = dk || dv || dS0;
+    if (g.parts > 1) {
+        int n = 0;
+        if (dq) g.r[n++] = rq;
+        if (back) g.r[n++] = rv;
+        hipError_t e = n ? launch_roles<T, false>(g, n, exact, s) : hipSuccess;
+        if (e == hipSuccess && n && g.joined) e = launch_join(g, n, s);
+        if (e != hipSuccess) return e;
+    }
     int n = 0;
     if (dq) g.r[n++] = rq;
     if (dk) g.r[n++] = rk;
-    if (K == M && (dv || dS0)) g.r[n++] = rv;   // equal widths: all in one launch
-    if (n) {
-        const hipError_t e = launch_roles(g, n, K == M ? 3 : 2, states, sh, ws, s);
+    if (n && dS0 && dS0 == dST && g.parts == 1) {   // dk's blocks read dST before dv's replace it
+        const hipError_t e = launch_roles<T, true>(g, n, exact, s);
         if (e != hipSuccess) return e;
+        n = 0;
     }
-    if (K != M && (dv || dS0)) {
-        g.r[0] = rv;
-        return launch_roles(g, 1, 1, states, sh, ws, s);
-    }
-    return hipSuccess;
+    if (dv || dS0) g.r[n++] = rv;
+    return n ? launch_roles<T, true>(g, n, exact, s) : hipSuccess;
 }
 
 }  // namespace
@@ -662,13 +829,9 @@ size_t linattn_workspace_bytes(DType t, const LinAttnShape &sh)
 {
     const int chunk = t == DType::BF16 ? Mat<bf16_t>::C : Mat<float>::C;
     const size_t state = (size_t)sh.B * sh.N * sh.K * sh.M * 4;
-    size_t most = 0;
-    for (int roles = 1; roles <= MAX_ROLES; ++roles)
-        for (const int dc : {sh.K, sh.M}) {
-            const SplitPlan p = split_plan(sh, chunk, roles, dc);
-            if (p.parts > 1 && p.parts * roles * state > most) most = p.parts * roles * state;
-        }
-    return most;
+    const int fwd = split_plan(sh, chunk, 1).parts, bwd = split_plan(sh, chunk, MAX_ROLES).parts;
+    const size_t f = fwd > 1 ? fwd * state : 0, b = bwd > 1 ? 2 * bwd * state : 0;
+    return f > b ? f : b;
 }
 
 hipError_t linattn_forward(DType t, const LinAttnShape &sh, const void *q, const void *k, const void *v,

@@ -437,6 +437,7 @@ __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(R
         waitcnt_vm<0>();   // this chunk's rows
         __syncthreads();   // everyone's; and the other buffer has been read
         if (t0 + C < end) issue(t0 + C, buf ^ 1);
+        if (col0 >= dc) continue;   // a wave beyond this role's columns only loads
         lds_char *tb = (lds_char *)lds + buf * chunk_bytes, *ta = tb + ABYTES;
         lds_char *tc = tb + (OUT ? 2 : 1) * ABYTES + wave * CBYTES;
         const int rows = min(C, end - t0);

@@ -341,6 +341,23 @@ LINATTN_CASES = [   # T, B, N, K, M, dtype, lengths, states, fused
     (1500, 2, 1, 128, 128, "bf16", None, True, True),
     (2100, 1, 1, 16, 32, "f32", "ragged", True, False),
     (50, 40, 16, 64, 64, "bf16", "ragged", False, True),   # many heads
+    # every padded width, in both sizes of a wave's columns, and key and value
+    # widths far apart (one launch pads them to the wider)
+    (70, 2, 2, 96, 80, "bf16", "ragged", True, False),
+    (70, 1, 2, 96, 96, "f32", None, True, True),
+    (100, 2, 1, 160, 136, "bf16", None, True, True),
+    (50, 1, 2, 160, 160, "f32", "ragged", True, False),
+    (66, 1, 1, 192, 24, "bf16", None, True, False),
+    (40, 2, 1, 184, 192, "f32", None, False, False),
+    (130, 1, 2, 224, 40, "bf16", "ragged", True, True),
+    (35, 1, 1, 8, 224, "f32", None, True, False),
+    (90, 1, 1, 248, 232, "f32", "ragged", True, True),
+    (34, 70, 16, 128, 96, "bf16", "ragged", True, False),
+    (20, 70, 16, 96, 112, "f32", None, True, True),
+    (17, 70, 16, 24, 32, "bf16", None, False, False),
+    (33, 70, 16, 16, 24, "f32", "ragged", True, False),
+    (400, 3, 8, 128, 128, "bf16", "ragged", True, True),   # parts joined by their blocks
+    (3000, 1, 1, 40, 256, "bf16", None, True, False),      # and by a launch of its own
 ]
 
 

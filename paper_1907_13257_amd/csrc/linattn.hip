@@ -322,18 +322,18 @@ __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(R
     // register only if it is said to be)
     const int n = __builtin_amdgcn_readfirstlane(sequence_length(g.lengths, b, g.T_));
     const int begin = part * g.part_len, stop = min(g.T_, begin + g.part_len), end = min(n, stop);
-    const int da = r.da, dc = r.dc, col0 = wave * WCOLS;
+    const int da = r.da, dc = r.dc, col0 = ((int)blockIdx.z * waves + wave) * WCOLS;
     T *const out = r.out;
     const long size = (long)da * dc, slots = bh * g.parts * size;
     const bool last = end >= n;   // of this sequence
     float *const XT = OUT && last && (n > 0 || part == 0) ? r.XT : nullptr;
 
-    if (!OUT && part == 0 && r.X0)   // the first state
+    if (!OUT && part == 0 && blockIdx.z == 0 && r.X0)   // the first state
         for (int i = threadIdx.x; i < size / 4; i += blockDim.x)
             reinterpret_cast<f32x4 *>(r.slots + slots)[i] = reinterpret_cast<const f32x4 *>(r.X0 + bh * size)[i];
     if (!OUT && last) return;
     if (OUT && !out && !XT) return;
-    if (OUT && out && n < stop) {   // behind the sequence's end
+    if (OUT && out && n < stop && blockIdx.z == 0) {   // behind the sequence's end
         const int per = dc * (int)sizeof(T) / 16, t0 = max(n, begin), all = (stop - t0) * per;
         for (int i = threadIdx.x; i < all; i += blockDim.x) {
             T *row = out + ((long)(t0 + i / per) * g.B + b) * r.ldo + (long)h * dc;
@@ -636,9 +636,11 @@ struct SplitPlan {
 // rows cost a wave the same for 16.  Where that leaves the SIMDs with less than
 // one wave each unsplit and few chunks in all (FEW_CHUNKS of a wave per SIMD),
 // time is the latency of a wave's chunks, and 16 columns halve it: 2 x 1999
-// tokens of 16 heads of 64 in 36 us with 32 columns and 29 with 16, 12 x 333 of
-// 5 heads in fp32, forward and backward, 90 and 75; but 128 x 50 tokens of 16
-// heads 52 and 67, 4 x 4096 of 16 heads of 128 467 and 526.
+// tokens of 16 heads of 64 in 36 us with 32 columns and 32 with 16, 12 x 333 of
+// 5 heads in fp32, forward and backward, 90 and 83; but 128 x 50 tokens of 16
+// heads 52 and 67, 4 x 4096 of 16 heads of 128 467 and 526.  Heads wider than
+// 128 always take 16: twice the state does not fit the registers.
+constexpr int MAX_WAVES = 8;   // of a block
 constexpr int TARGET_WAVES = 2048, MIN_CHUNKS = 3, FEW_CHUNKS = 16, SIMDS = 1024;
 SplitPlan split_plan(const LinAttnShape &sh, int chunk, int roles)
 {
@@ -650,8 +652,8 @@ SplitPlan split_plan(const LinAttnShape &sh, int chunk, int roles)
     if (parts > most) parts = most;
     if (parts < 1) parts = 1;
     const int per = (int)((chunks + parts - 1) / parts);
-    const bool few = waves < SIMDS && waves * chunks < (long)FEW_CHUNKS * SIMDS && width <= 128;
-    return SplitPlan{(chunks + per - 1) / per, per * chunk, few ? 1 : 2};
+    const bool few = waves < SIMDS && waves * chunks < (long)FEW_CHUNKS * SIMDS;
+    return SplitPlan{(chunks + per - 1) / per, per * chunk, few || width > 128 ? 1 : 2};
 }
 
 template <typename T, int DA, bool OUT, int NP, int MT>
@@ -659,14 +661,15 @@ hipError_t launch_chunks(const Roles<T> &g, int roles, int width, hipStream_t s)
 {
     constexpr int WCOLS = 16 * MT;
     constexpr int C = Mat<T>::C, CHA = row_chunks<T, DA>(), CHC = WCOLS * (int)sizeof(T) / 16;
-    const int waves = (width + WCOLS - 1) / WCOLS;
+    const int columns = (width + WCOLS - 1) / WCOLS, blocks = (columns + MAX_WAVES - 1) / MAX_WAVES;
+    const int waves = (columns + blocks - 1) / blocks;   // of a block; the columns of a head may take two
     const int lds = 2 * (C * CHA / 64 * (OUT ? 2 : 1) * Tile<CHA>::PITCH + C * CHC / 64 * waves * Tile<CHC>::PITCH);
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(linattn_chunks_kernel<T, DA, OUT, NP, MT>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((linattn_chunks_kernel<T, DA, OUT, NP, MT>), dim3((unsigned)((long)g.B * g.N * g.parts), roles),
+    hipLaunchKernelGGL((linattn_chunks_kernel<T, DA, OUT, NP, MT>), dim3((unsigned)((long)g.B * g.N * g.parts), roles, blocks),
                        dim3(64 * waves), lds, s, g);
     return hipGetLastError();
 }
@@ -686,10 +689,10 @@ hipError_t launch_width(const Roles<T> &g, int roles, hipStream_t s)
     case 2: return one ? launch_chunks<T, 64, OUT, NP, 1>(g, roles, dc, s) : launch_chunks<T, 64, OUT, NP, 2>(g, roles, dc, s);
     case 3: return one ? launch_chunks<T, 96, OUT, NP, 1>(g, roles, dc, s) : launch_chunks<T, 96, OUT, NP, 2>(g, roles, dc, s);
     case 4: return one ? launch_chunks<T, 128, OUT, NP, 1>(g, roles, dc, s) : launch_chunks<T, 128, OUT, NP, 2>(g, roles, dc, s);
-    case 5: return launch_chunks<T, 160, OUT, NP, 2>(g, roles, dc, s);
-    case 6: return launch_chunks<T, 192, OUT, NP, 2>(g, roles, dc, s);
-    case 7: return launch_chunks<T, 224, OUT, NP, 2>(g, roles, dc, s);
-    default: return launch_chunks<T, 256, OUT, NP, 2>(g, roles, dc, s);
+    case 5: return launch_chunks<T, 160, OUT, NP, 1>(g, roles, dc, s);
+    case 6: return launch_chunks<T, 192, OUT, NP, 1>(g, roles, dc, s);
+    case 7: return launch_chunks<T, 224, OUT, NP, 1>(g, roles, dc, s);
+    default: return launch_chunks<T, 256, OUT, NP, 1>(g, roles, dc, s);
     }
 }
 

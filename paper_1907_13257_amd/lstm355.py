@@ -400,57 +400,63 @@ class Layer:
         return lstm_describe_tiling(self.handle)
 
 
-def _rows_ptr(t, what, dtype, rows, width, ld, device, optional=False):
-    """The address of a tensor on GPU `device` that holds `rows` rows of `width`
-    elements, `ld` elements apart, after checking that it does (its leading
-    dimensions are the rows, however many there are)."""
-    if t is None:
-        if optional:
-            return None
-        raise ValueError(f"{what} is required")
-    if isinstance(t, int):
-        return t
-    if t.dtype is not dtype:
-        raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
-    if t.get_device() != device:
-        raise ValueError(f"{what} is on {t.device}, the operator on cuda:{device}")
-    if ld == width and t.is_contiguous() and t.numel() == rows * width and t.dim() and t.size(-1) == width:
+def _rows_arg(what, dtype, rows, width, ld, gpu, optional=False):
+    """A function that gives the address of a tensor on GPU `gpu` holding `rows`
+    rows of `width` elements, `ld` elements apart (its leading dimensions are
+    the rows, however many there are), after checking that it does.  Addresses
+    pass through; None does where the argument is optional."""
+    n, dense = rows * width, ld == width
+
+    def address(t):
+        if t is None or t.__class__ is int:
+            if t is None and not optional:
+                raise ValueError(f"{what} is required")
+            return t
+        if t.dtype is not dtype:
+            raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
+        if t.get_device() != gpu:
+            raise ValueError(f"{what} is on {t.device}, the operator on cuda:{gpu}")
+        if dense and t.is_contiguous() and t.numel() == n and t.dim() and t.size(-1) == width:
+            return t.data_ptr()
+        shape = t.shape
+        found, expect = 1, ld
+        ok = bool(shape) and shape[-1] == width and (width == 1 or t.stride(-1) == 1)
+        for dim in range(len(shape) - 2, -1, -1):
+            ok = ok and (shape[dim] == 1 or t.stride(dim) == expect)
+            found *= shape[dim]
+            expect *= shape[dim]
+        if not ok or found != rows:
+            raise ValueError(f"{what} must be {rows} rows of {width} elements, {ld} apart: got shape {tuple(shape)}, "
+                             f"strides {t.stride()}")
         return t.data_ptr()
-    shape = t.shape
-    n, expect = 1, ld
-    ok = bool(shape) and shape[-1] == width and (width == 1 or t.stride(-1) == 1)
-    for dim in range(len(shape) - 2, -1, -1):
-        ok = ok and (shape[dim] == 1 or t.stride(dim) == expect)
-        n *= shape[dim]
-        expect *= shape[dim]
-    if not ok or n != rows:
-        raise ValueError(f"{what} must be {rows} rows of {width} elements, {ld} apart: got shape {tuple(shape)}, "
-                         f"strides {t.stride()}")
-    return t.data_ptr()
+
+    return address
 
 
-def _vector_ptr(t, what, dtype, n, device, optional=False):
+def _vector_arg(what, dtype, n, gpu, optional=False):
     """The same for n contiguous elements of any shape."""
-    if t is None:
-        if optional:
-            return None
-        raise ValueError(f"{what} is required")
-    if isinstance(t, int):
-        return t
-    if t.dtype is not dtype:
-        raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
-    if t.get_device() != device:
-        raise ValueError(f"{what} is on {t.device}, the operator on cuda:{device}")
-    if t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{what} must be {n} contiguous elements, got shape {tuple(t.shape)}, strides {t.stride()}")
-    return t.data_ptr()
+
+    def address(t):
+        if t is None or t.__class__ is int:
+            if t is None and not optional:
+                raise ValueError(f"{what} is required")
+            return t
+        if t.dtype is not dtype:
+            raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
+        if t.get_device() != gpu:
+            raise ValueError(f"{what} is on {t.device}, the operator on cuda:{gpu}")
+        if t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{what} must be {n} contiguous elements, got shape {tuple(t.shape)}, strides {t.stride()}")
+        return t.data_ptr()
+
+    return address
 
 
 class _Operator:
     """What the operators' classes share: the device they were made on, their
     workspace, and the stream of a call.  Calls of one object that overlap (on
     several streams) would share its workspace: order them, or make an object
-    for each."""
+    for each.  The checks of a call's tensors are made once, as functions."""
 
     def __init__(self, dtype, device, workspace_bytes):
         import torch
@@ -466,7 +472,6 @@ class _Operator:
         # the current stream's handle without a Stream object around it (2.7 us
         # less per call), where this torch offers it
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        self._float, self._int32, self._int64 = torch.float32, torch.int32, torch.int64
         self.workspace = torch.empty(workspace_bytes, dtype=torch.uint8, device=self.device)
         self.ws_ptr, self.ws_bytes = (self.workspace.data_ptr() if workspace_bytes else None), workspace_bytes
         self.lib = load_library()
@@ -478,14 +483,11 @@ class _Operator:
             return self._raw_stream(self.gpu)
         return _stream(stream)
 
-    def _rows(self, t, what, rows, width, ld=None, optional=False):
-        return _rows_ptr(t, what, self.torch_dtype, rows, width, width if ld is None else ld, self.gpu, optional)
+    def _rows(self, what, rows, width, ld=None, optional=False, dtype=None):
+        return _rows_arg(what, dtype or self.torch_dtype, rows, width, ld or width, self.gpu, optional)
 
-    def _f32(self, t, what, rows, width, optional=False):
-        return _rows_ptr(t, what, self._float, rows, width, width, self.gpu, optional)
-
-    def _vector(self, t, what, dtype, n, optional=False):
-        return _vector_ptr(t, what, dtype, n, self.gpu, optional)
+    def _vector(self, what, dtype, n, optional=False):
+        return _vector_arg(what, dtype, n, self.gpu, optional)
 
 
 class Embedding(_Operator):
@@ -495,21 +497,22 @@ class Embedding(_Operator):
 
     def __init__(self, N, V, D, dtype="bf16", scale=1.0, ldo=0, device="cuda"):
         super().__init__(dtype, device, lstm_embed_workspace_size(N, V, D))
+        import torch
         self.N, self.V, self.D, self.scale, self.ldo = N, V, D, float(scale), ldo or D
+        self._ids = self._vector("ids", torch.int64, N)
+        self._table, self._dtable = self._rows("table", V, D), self._rows("dtable", V, D, dtype=torch.float32)
+        self._out, self._dout = self._rows("out", N, D, ldo), self._rows("dout", N, D, ldo)
 
     def forward(self, ids, table, out, stream=None):
-        _check(self.lib.lstm_embed_forward(self.code, self.N, self.V, self.D,
-                                           self._vector(ids, "ids", self._int64, self.N),
-                                           self._rows(table, "table", self.V, self.D), self.scale,
-                                           self._rows(out, "out", self.N, self.D, self.ldo), self.ldo,
-                                           self._stream(stream)), "lstm_embed_forward")
+        st = self.lib.lstm_embed_forward(self.code, self.N, self.V, self.D, self._ids(ids), self._table(table),
+                                         self.scale, self._out(out), self.ldo, self._stream(stream))
+        _check(st, "lstm_embed_forward")
 
     def backward(self, ids, dout, dtable, accumulate=False, stream=None):
-        _check(self.lib.lstm_embed_backward(self.code, self.N, self.V, self.D,
-                                            self._vector(ids, "ids", self._int64, self.N),
-                                            self._rows(dout, "dout", self.N, self.D, self.ldo), self.ldo, self.scale,
-                                            self._f32(dtable, "dtable", self.V, self.D), int(bool(accumulate)),
-                                            self.ws_ptr, self.ws_bytes, self._stream(stream)), "lstm_embed_backward")
+        st = self.lib.lstm_embed_backward(self.code, self.N, self.V, self.D, self._ids(ids), self._dout(dout), self.ldo,
+                                          self.scale, self._dtable(dtable), int(bool(accumulate)), self.ws_ptr,
+                                          self.ws_bytes, self._stream(stream))
+        _check(st, "lstm_embed_backward")
 
 
 class AddNorm(_Operator):
@@ -522,38 +525,33 @@ class AddNorm(_Operator):
         import torch
         self.rows, self.D, self.eps = rows, D, float(eps)
         self.ldx, self.ldr, self.ldy = ldx or D, ldr or D, ldy or D
-        self._eight = (torch.float8_e4m3fn, torch.uint8)
+        self._x, self._res = self._rows("x", rows, D, ldx), self._rows("res", rows, D, ldr, True)
+        self._sum, self._kept = self._rows("sum", rows, D, ldr, True), self._rows("sum", rows, D, ldr)
+        self._y, self._dy = self._rows("y", rows, D, ldy), self._rows("dy", rows, D, ldy)
+        self._dsum, self._dx = self._rows("dsum", rows, D, ldr, True), self._rows("dx", rows, D, ldx)
+        self._g, self._dg = self._vector("g", self.torch_dtype, D), self._vector("dg", torch.float32, D)
+        self._scale, self._uint8 = self._vector("scale", torch.float32, rows), torch.uint8
+        self._y8 = self._rows("y8", rows, D, dtype=torch.float8_e4m3fn)
+        self._bits = self._rows("y8", rows, D, dtype=torch.uint8)
 
     def forward(self, x, res, g, sum, y, stream=None):
-        R, D = self.rows, self.D
-        _check(self.lib.lstm_add_norm(self.code, R, D, self._rows(x, "x", R, D, self.ldx), self.ldx,
-                                      self._rows(res, "res", R, D, self.ldr, True), self.ldr,
-                                      self._vector(g, "g", self.torch_dtype, D), self.eps,
-                                      self._rows(sum, "sum", R, D, self.ldr, True),
-                                      self._rows(y, "y", R, D, self.ldy), self.ldy, self._stream(stream)),
-               "lstm_add_norm")
+        st = self.lib.lstm_add_norm(self.code, self.rows, self.D, self._x(x), self.ldx, self._res(res), self.ldr,
+                                    self._g(g), self.eps, self._sum(sum), self._y(y), self.ldy, self._stream(stream))
+        _check(st, "lstm_add_norm")
 
     def forward_q8(self, x, res, g, sum, y8, scale, stream=None):
-        R, D = self.rows, self.D
-        eight = self._eight[1] if getattr(y8, "dtype", None) is self._eight[1] else self._eight[0]
-        _check(self.lib.lstm_add_norm_q8(self.code, R, D, self._rows(x, "x", R, D, self.ldx), self.ldx,
-                                         self._rows(res, "res", R, D, self.ldr, True), self.ldr,
-                                         self._vector(g, "g", self.torch_dtype, D), self.eps,
-                                         self._rows(sum, "sum", R, D, self.ldr, True),
-                                         _rows_ptr(y8, "y8", eight, R, D, D, self.gpu),
-                                         self._vector(scale, "scale", self._float, R), self._stream(stream)),
-               "lstm_add_norm_q8")
+        eight = self._bits if getattr(y8, "dtype", None) is self._uint8 else self._y8
+        st = self.lib.lstm_add_norm_q8(self.code, self.rows, self.D, self._x(x), self.ldx, self._res(res), self.ldr,
+                                       self._g(g), self.eps, self._sum(sum), eight(y8), self._scale(scale),
+                                       self._stream(stream))
+        _check(st, "lstm_add_norm_q8")
 
     def backward(self, dy, dsum, sum, g, dx, dg, accumulate=False, stream=None):
-        R, D = self.rows, self.D
-        _check(self.lib.lstm_add_norm_backward(self.code, R, D, self._rows(dy, "dy", R, D, self.ldy), self.ldy,
-                                               self._rows(dsum, "dsum", R, D, self.ldr, True),
-                                               self._rows(sum, "sum", R, D, self.ldr), self.ldr,
-                                               self._vector(g, "g", self.torch_dtype, D), self.eps,
-                                               self._rows(dx, "dx", R, D, self.ldx), self.ldx,
-                                               self._vector(dg, "dg", self._float, D), int(bool(accumulate)),
-                                               self.ws_ptr, self.ws_bytes, self._stream(stream)),
-               "lstm_add_norm_backward")
+        st = self.lib.lstm_add_norm_backward(self.code, self.rows, self.D, self._dy(dy), self.ldy, self._dsum(dsum),
+                                             self._kept(sum), self.ldr, self._g(g), self.eps, self._dx(dx), self.ldx,
+                                             self._dg(dg), int(bool(accumulate)), self.ws_ptr, self.ws_bytes,
+                                             self._stream(stream))
+        _check(st, "lstm_add_norm_backward")
 
 
 class LinearAttention(_Operator):
@@ -567,45 +565,39 @@ class LinearAttention(_Operator):
         scale = K ** -0.5 if scale is None else float(scale)
         self.desc = lstm_linattn_desc(T, B, heads, K, M, dtype, scale, ldq, ldk, ldv, ldo)
         super().__init__(dtype, device, lstm_linattn_workspace_size(self.desc))
+        import torch
         self.T, self.B, self.heads, self.K, self.M, self.scale = T, B, heads, K, M, scale
-        self.ldq, self.ldk = ldq or heads * K, ldk or heads * K
-        self.ldv, self.ldo = ldv or heads * M, ldo or heads * M
         self._desc = ctypes.byref(self.desc)
-
-    def _state(self, t, what, optional=True):
-        return _vector_ptr(t, what, self._float, self.B * self.heads * self.K * self.M, self.gpu, optional)
-
-    def _inputs(self, q, k, v, decay):
-        rows, hk, hm = self.T * self.B, self.heads * self.K, self.heads * self.M
-        return (self._rows(q, "q", rows, hk, self.ldq), self._rows(k, "k", rows, hk, self.ldk),
-                self._rows(v, "v", rows, hm, self.ldv), self._vector(decay, "decay", self._float, self.heads))
+        rows, hk, hm, states = T * B, heads * K, heads * M, B * heads * K * M
+        self._q, self._k, self._v = (self._rows("q", rows, hk, ldq), self._rows("k", rows, hk, ldk),
+                                     self._rows("v", rows, hm, ldv))
+        self._o, self._do = self._rows("o", rows, hm, ldo), self._rows("do", rows, hm, ldo)
+        self._dq, self._dk, self._dv = (self._rows("dq", rows, hk, ldq, True), self._rows("dk", rows, hk, ldk, True),
+                                        self._rows("dv", rows, hm, ldv, True))
+        self._decay = self._vector("decay", torch.float32, heads)
+        self._lengths = self._vector("lengths", torch.int32, B, True)
+        self._S, self._S_out = self._vector("S", torch.float32, states), self._vector("S_out", torch.float32, states)
+        self._S0, self._ST, self._dST, self._dS0 = (self._vector(n, torch.float32, states, True)
+                                                    for n in ("S0", "ST", "dST", "dS0"))
 
     def forward(self, q, k, v, decay, o, lengths=None, S0=None, ST=None, stream=None):
-        _check(self.lib.lstm_linattn_forward(self._desc, *self._inputs(q, k, v, decay),
-                                             self._vector(lengths, "lengths", self._int32, self.B, True),
-                                             self._state(S0, "S0"),
-                                             self._rows(o, "o", self.T * self.B, self.heads * self.M, self.ldo),
-                                             self._state(ST, "ST"), self.ws_ptr, self.ws_bytes, self._stream(stream)),
-               "lstm_linattn_forward")
+        st = self.lib.lstm_linattn_forward(self._desc, self._q(q), self._k(k), self._v(v), self._decay(decay),
+                                           self._lengths(lengths), self._S0(S0), self._o(o), self._ST(ST), self.ws_ptr,
+                                           self.ws_bytes, self._stream(stream))
+        _check(st, "lstm_linattn_forward")
 
     def backward(self, do, q, k, v, decay, dq, dk, dv, lengths=None, S0=None, dST=None, dS0=None, stream=None):
-        rows, hk, hm = self.T * self.B, self.heads * self.K, self.heads * self.M
-        _check(self.lib.lstm_linattn_backward(self._desc, self._rows(do, "do", rows, hm, self.ldo),
-                                              *self._inputs(q, k, v, decay),
-                                              self._vector(lengths, "lengths", self._int32, self.B, True),
-                                              self._state(S0, "S0"), self._state(dST, "dST"),
-                                              self._rows(dq, "dq", rows, hk, self.ldq, True),
-                                              self._rows(dk, "dk", rows, hk, self.ldk, True),
-                                              self._rows(dv, "dv", rows, hm, self.ldv, True),
-                                              self._state(dS0, "dS0"), self.ws_ptr, self.ws_bytes,
-                                              self._stream(stream)), "lstm_linattn_backward")
+        st = self.lib.lstm_linattn_backward(self._desc, self._do(do), self._q(q), self._k(k), self._v(v),
+                                            self._decay(decay), self._lengths(lengths), self._S0(S0), self._dST(dST),
+                                            self._dq(dq), self._dk(dk), self._dv(dv), self._dS0(dS0), self.ws_ptr,
+                                            self.ws_bytes, self._stream(stream))
+        _check(st, "lstm_linattn_backward")
 
     def step(self, q, k, v, decay, S, S_out, o, lengths=None, stream=None):
-        _check(self.lib.lstm_linattn_step(self._desc, *self._inputs(q, k, v, decay),
-                                          self._vector(lengths, "lengths", self._int32, self.B, True),
-                                          self._state(S, "S", False), self._state(S_out, "S_out", False),
-                                          self._rows(o, "o", self.T * self.B, self.heads * self.M, self.ldo),
-                                          self._stream(stream)), "lstm_linattn_step")
+        st = self.lib.lstm_linattn_step(self._desc, self._q(q), self._k(k), self._v(v), self._decay(decay),
+                                        self._lengths(lengths), self._S(S), self._S_out(S_out), self._o(o),
+                                        self._stream(stream))
+        _check(st, "lstm_linattn_step")
 
 
 class StackLayer:

@@ -337,7 +337,10 @@ lstm_status_t lstm_add_norm_backward(lstm_dtype_t dtype, long rows, int D, const
  *   q, k [T][B][N*K], v, o [T][B][N*M] (head n in columns n*K.. or n*M..), row
  *   strides ldq, ldk, ldv, ldo between consecutive (t,b) rows: columns of one
  *   fused projection may be given.  decay [N] fp32, every value in 0 .. 1
- *   (constants of the layer: they get no gradient).  States [B][N][K][M] fp32. */
+ *   (constants of the layer: they get no gradient).  States [B][N][K][M] fp32.
+ * A value that is not finite spreads within its sequence and head only, but
+ * there also to outputs up to 31 steps before it (a chunk's sum multiplies what
+ * it leaves out by zero). */
 typedef struct {
     int T, B, N;          /* steps, batch rows, heads */
     int K, M;             /* key and value width of a head: multiples of 8, 8 .. 256 */

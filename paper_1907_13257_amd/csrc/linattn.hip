@@ -334,9 +334,10 @@ __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(R
     if (!OUT && last) return;
     if (OUT && !out && !XT) return;
     if (OUT && out && n < stop && blockIdx.z == 0) {   // behind the sequence's end
-        const int per = dc * (int)sizeof(T) / 16, t0 = max(n, begin), all = (stop - t0) * per;
-        for (int i = threadIdx.x; i < all; i += blockDim.x) {
-            T *row = out + ((long)(t0 + i / per) * g.B + b) * r.ldo + (long)h * dc;
+        const int per = dc * (int)sizeof(T) / 16, t0 = max(n, begin);
+        const long all = (long)(stop - t0) * per;
+        for (long i = threadIdx.x; i < all; i += blockDim.x) {
+            T *row = out + ((t0 + i / per) * g.B + b) * r.ldo + (long)h * dc;
             reinterpret_cast<u32x4 *>(row)[i % per] = zero16();
         }
     }
@@ -422,7 +423,8 @@ __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(R
     float whole = 1.0f;   // the state's factor over that chunk
     // The state is gain * X: a chunk's decay goes into gain, its tokens are
     // added divided by gain, and X is multiplied only when gain gets small
-    // (one chunk in many for the usual decays)
+    // (one chunk in many for the usual decays; so X is at most 2^10 times the
+    // state)
     float gain = 1.0f;
 
     Reader<CHA, T> ra;
@@ -546,7 +548,7 @@ __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(R
                 }
             }
             gain *= whole;
-            if (__builtin_amdgcn_readfirstlane(gain < 0x1p-20f)) {
+            if (__builtin_amdgcn_readfirstlane(gain < 0x1p-10f)) {
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt)
 #pragma unroll

@@ -9,6 +9,17 @@ using namespace lstm355;
 
 namespace {
 
+// The status of a launch; nothing is thrown across the C boundary.
+template <typename F>
+lstm_status_t launched(const char *what, F launch)
+{
+    try {
+        return hip_status(what, launch());
+    } catch (...) {
+        return invalid("exception");
+    }
+}
+
 constexpr long MAX_INDEX = (1L << 31) - (1L << 20);   // rows of a table, tokens of a call: 32-bit positions
 
 bool known(lstm_dtype_t t) { return t == LSTM_F32 || t == LSTM_BF16; }
@@ -58,8 +69,9 @@ lstm_status_t add_norm_any(lstm_dtype_t dtype, long rows, int D, const void *x, 
     if (scale && !aligned4(scale)) return invalid("fp32 tensors must be 4-byte aligned");
     if (sum && sum == x && ldx != ldr) return invalid("sum may be x only when ldx = ldr");
     const NormArgs a{rows, D, x, res, g, ldx, ldr, ldy, eps, sum, y, scale};
-    TRY_HIP("add_norm", add_norm(dtype_of(dtype), a, static_cast<hipStream_t>(stream)));
-    return LSTM_OK;
+    return launched("add_norm", [&] {
+        return add_norm(dtype_of(dtype), a, static_cast<hipStream_t>(stream));
+    });
 }
 
 lstm_status_t check_linattn(const lstm_linattn_desc_t *d, LinAttnShape *sh)
@@ -114,9 +126,9 @@ extern "C" lstm_status_t lstm_embed_forward(lstm_dtype_t dtype, long N, long V, 
     for (const void *p : {table, (const void *)out})
         if (!aligned16(p)) return invalid("device tensors must be 16-byte aligned");
     if (!aligned8(ids)) return invalid("ids must be 8-byte aligned");
-    TRY_HIP("embed_forward", embed_forward(dtype_of(dtype), N, V, D, ids, table, scale, out, ld,
-                                           static_cast<hipStream_t>(stream)));
-    return LSTM_OK;
+    return launched("embed_forward", [&] {
+        return embed_forward(dtype_of(dtype), N, V, D, ids, table, scale, out, ld, static_cast<hipStream_t>(stream));
+    });
 }
 
 extern "C" size_t lstm_embed_workspace_size(long N, long V, int D)
@@ -140,9 +152,10 @@ extern "C" lstm_status_t lstm_embed_backward(lstm_dtype_t dtype, long N, long V,
     if (!aligned8(ids)) return invalid("ids must be 8-byte aligned");
     st = check_workspace(workspace, workspace_bytes, embed_workspace_bytes(N, V, D));
     if (st != LSTM_OK) return st;
-    TRY_HIP("embed_backward", embed_backward(dtype_of(dtype), N, V, D, ids, dout, ld, scale, dtable, accumulate,
-                                             workspace, static_cast<hipStream_t>(stream)));
-    return LSTM_OK;
+    return launched("embed_backward", [&] {
+        return embed_backward(dtype_of(dtype), N, V, D, ids, dout, ld, scale, dtable, accumulate, workspace,
+                              static_cast<hipStream_t>(stream));
+    });
 }
 
 extern "C" lstm_status_t lstm_add_norm(lstm_dtype_t dtype, long rows, int D, const void *x, long ldx, const void *res,
@@ -181,8 +194,9 @@ extern "C" lstm_status_t lstm_add_norm_backward(lstm_dtype_t dtype, long rows, i
     st = check_workspace(workspace, workspace_bytes, norm_partial_floats(rows, D) * 4);
     if (st != LSTM_OK) return st;
     const NormBwdArgs a{rows, D, dy, dsum, sum, g, ldx, ldr, ldy, eps, dx, dg, accumulate, static_cast<float *>(workspace)};
-    TRY_HIP("add_norm_backward", add_norm_backward(dtype_of(dtype), a, static_cast<hipStream_t>(stream)));
-    return LSTM_OK;
+    return launched("add_norm_backward", [&] {
+        return add_norm_backward(dtype_of(dtype), a, static_cast<hipStream_t>(stream));
+    });
 }
 
 extern "C" size_t lstm_linattn_workspace_size(const lstm_linattn_desc_t *d)
@@ -200,9 +214,10 @@ extern "C" lstm_status_t lstm_linattn_forward(const lstm_linattn_desc_t *d, cons
     if (st == LSTM_OK) st = check_linattn_pointers({q, k, v, o}, {S0, ST}, decay, lengths);
     if (st == LSTM_OK) st = check_workspace(workspace, workspace_bytes, linattn_workspace_bytes(dtype_of(d->dtype), sh));
     if (st != LSTM_OK) return st;
-    TRY_HIP("linattn_forward", linattn_forward(dtype_of(d->dtype), sh, q, k, v, decay, lengths, S0, o, ST, workspace,
-                                               static_cast<hipStream_t>(stream)));
-    return LSTM_OK;
+    return launched("linattn_forward", [&] {
+        return linattn_forward(dtype_of(d->dtype), sh, q, k, v, decay, lengths, S0, o, ST, workspace,
+                               static_cast<hipStream_t>(stream));
+    });
 }
 
 extern "C" lstm_status_t lstm_linattn_backward(const lstm_linattn_desc_t *d, const void *d_o, const void *q,
@@ -215,9 +230,10 @@ extern "C" lstm_status_t lstm_linattn_backward(const lstm_linattn_desc_t *d, con
     if (st == LSTM_OK) st = check_linattn_pointers({d_o, q, k, v}, {S0, dST, dq, dk, dv, dS0}, decay, lengths);
     if (st == LSTM_OK) st = check_workspace(workspace, workspace_bytes, linattn_workspace_bytes(dtype_of(d->dtype), sh));
     if (st != LSTM_OK) return st;
-    TRY_HIP("linattn_backward", linattn_backward(dtype_of(d->dtype), sh, d_o, q, k, v, decay, lengths, S0, dST, dq, dk,
-                                                 dv, dS0, workspace, static_cast<hipStream_t>(stream)));
-    return LSTM_OK;
+    return launched("linattn_backward", [&] {
+        return linattn_backward(dtype_of(d->dtype), sh, d_o, q, k, v, decay, lengths, S0, dST, dq, dk, dv, dS0,
+                                workspace, static_cast<hipStream_t>(stream));
+    });
 }
 
 extern "C" lstm_status_t lstm_linattn_step(const lstm_linattn_desc_t *d, const void *q, const void *k, const void *v,
@@ -229,7 +245,8 @@ extern "C" lstm_status_t lstm_linattn_step(const lstm_linattn_desc_t *d, const v
     if (st == LSTM_OK && sh.T != 1) st = invalid("a step takes one token: T must be 1");
     if (st == LSTM_OK) st = check_linattn_pointers({q, k, v, o, S, S_out}, {}, decay, lengths);
     if (st != LSTM_OK) return st;
-    TRY_HIP("linattn_step", linattn_step(dtype_of(d->dtype), sh, q, k, v, decay, lengths, S, S_out, o,
-                                         static_cast<hipStream_t>(stream)));
-    return LSTM_OK;
+    return launched("linattn_step", [&] {
+        return linattn_step(dtype_of(d->dtype), sh, q, k, v, decay, lengths, S, S_out, o,
+                            static_cast<hipStream_t>(stream));
+    });
 }

@@ -63,6 +63,8 @@ EMBED_CASES = [   # N, V, D, dtype, ldo, ids
     (1025, 2047, 8, "bf16", 0, "mixed"),     # one digit
     (6400, 32000, 1024, "bf16", 0, "zipf"),
     (5000, 300, 136, "f32", 0, "zipf"),
+    (8192, 40, 16, "f32", 0, "zipf"),        # the most tokens that are ranked outright
+    (8193, 40, 16, "f32", 0, "zipf"),        # the fewest that are not
     (9001, 5000000, 8, "bf16", 0, "mixed"),  # three digits
     (70001, 1000, 24, "bf16", 0, "zipf"),    # a row of some ten thousand tokens
     (300000, 100003, 8, "f32", 0, "mixed"),  # blocks of several tiles
@@ -604,6 +606,28 @@ def test_linattn_gradients_by_differences():
         limit = linattn_roundings(c, T, K, M) * U * (su + sd + size)
         announce(f"differences of {n}: {abs((up - down) / 2 - want):.2e} of {limit:.2e}")
         assert abs((up - down) / 2 - want) <= limit
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_linattn_keeps_what_is_not_finite_to_its_head(dtype):
+    """A NaN and an infinity in one head of one row leave every other head and
+    row as they are, bit for bit, in both directions."""
+    T, B, N, K, M = 100, 2, 3, 32, 48
+    c = linattn_case(T, B, N, K, M, dtype, None, True)
+    op = make_linattn(T, B, N, K, M, dtype, False)
+    want = {n: x.clone() for n, x in run_linattn(op, device_buffers(c, T, B, N, K, M, dtype, False)).items()}
+    d = device_buffers(c, T, B, N, K, M, dtype, False)
+    d["k"][50, 1, 2 * K + 3] = float("nan")
+    d["v"][60, 1, 2 * M + 5] = float("inf")
+    got = run_linattn(op, d)
+    for n, x in got.items():
+        if n in ("ST", "dS0"):
+            x, w = x.reshape(B * N, -1), want[n].reshape(B * N, -1)
+        else:
+            x, w = (t.view(T, B * N, -1).transpose(0, 1) for t in (x, want[n]))
+        assert torch.equal(x[:B * N - 1], w[:B * N - 1]), n
+    assert torch.equal(got["o"][:32, 1], want["o"][:32, 1])   # more than a chunk before it
+    assert got["o"][50:, 1, 2 * M:].isnan().any()
 
 
 def test_linattn_beyond_32_bit_offsets():

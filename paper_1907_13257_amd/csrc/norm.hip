@@ -71,8 +71,10 @@ __device__ __forceinline__ Sum2 reduce_row(Sum2 v, float *red)
 }
 
 // A row is held in registers by W waves, P vectors per thread (thread t has
-// vectors t, t + 64 W, ...).  Blocks of W <= 4 waves per row: 4 / W rows at
-// a time in W = 1, one otherwise.
+// vectors t, t + 64 W, ...), so it is read once and both sums over it need no
+// second pass.  A block has four rows where a row is one wave's, else one.
+// Bound by memory: 6400 rows of 1024 bf16 in 8.8 us (52 MB, 5.9 TB/s), 20001 of
+// 8192 with the 8-bit output in 211 us (1.15 GB, 5.4 TB/s); 16 rows in 3.4 us.
 template <int W> constexpr int ROWS = W == 1 ? 4 : 1;
 template <int W> constexpr int THREADS = W == 1 ? 256 : W * 64;
 
@@ -152,7 +154,8 @@ __global__ __launch_bounds__(THREADS<W>) void add_norm_kernel(NormArgs a, int nv
 }
 
 // dx = dsum + rho g dy - s rho^3 mean(g dy s); a block adds dy s rho of its
-// rows (a fixed set) in registers and leaves its sums in `partial`.
+// rows (a fixed set) in registers and leaves its sums in `partial`.  Bound by
+// memory: 6400 rows of 1024 bf16 in 10.7 us (52 MB, 4.9 TB/s).
 template <typename T, int W, int P>
 __global__ __launch_bounds__(THREADS<W>) void add_norm_backward_kernel(NormBwdArgs a, int nv)
 {
@@ -231,7 +234,8 @@ __global__ __launch_bounds__(THREADS<W>) void add_norm_backward_kernel(NormBwdAr
 }
 
 // dg (+)= the sum of the blocks' rows: 32 groups of 16 lanes take every 32nd
-// row of 64 columns, and their sums are added in order.
+// row of 64 columns, and their sums are added in order.  3.0 us for 1024
+// columns, the latency of a launch and 16 loads; one thread per column took 234.
 __global__ __launch_bounds__(512) void norm_gain_kernel(const float *__restrict__ partial, int rows, int D,
                                                         float *__restrict__ dg, int accumulate)
 {
@@ -253,6 +257,8 @@ __global__ __launch_bounds__(512) void norm_gain_kernel(const float *__restrict_
 }
 
 // Blocks of the backward pass, each of which leaves one row of partial sums.
+// Forward and backward with 256, 512, 1024 blocks: 6400 rows of 1024 33.5, 28.4,
+// 28.9 us, of 4096 110, 86, 86, 40000 rows of 1024 150, 126, 129.
 constexpr int BWD_BLOCKS = 512;
 
 int bwd_blocks(long rows, int rows_per_block)
@@ -286,11 +292,15 @@ hipError_t launch_norm_bwd(const NormBwdArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-// Waves and vectors per thread of a row of nv vectors.
+// Waves and vectors per thread of a row of nv vectors: one wave as long as it
+// has the row in two vectors per lane, since four waves meet at barriers and a
+// quarter of a wave's rows are in flight.  6400 rows forward and backward with
+// one wave and with four: 1024 bf16 (128 vectors) 28 and 39 us, 2048 56 and 51,
+// 4096 147 and 86.
 #define NORM_BY_WIDTH(CALL)                    \
     if (nv <= 64) return CALL(1, 1);           \
     if (nv <= 128) return CALL(1, 2);          \
-    if (nv <= 256) return CALL(1, 4);          \
+    if (nv <= 256) return CALL(4, 1);          \
     if (nv <= 512) return CALL(4, 2);          \
     if (nv <= 1024) return CALL(4, 4);         \
     if (nv <= 2048) return CALL(8, 4);         \

@@ -182,6 +182,8 @@ NORM_CASES = [   # rows, D, dtype, extra columns between rows, residual, scale o
     (1025, 72, "bf16", 0, True, 1.0),   # more rows than partial sums
     (5001, 264, "f32", 0, True, 1.0),
     (7, 1024, "bf16", 0, False, 1.0),
+    (37, 2048, "bf16", 0, True, 1.0),   # the widest and the narrowest row of a number of waves
+    (19, 1024, "f32", 8, False, 1.0),
     (33, 2056, "bf16", 0, True, 1.0),
     (9, 4104, "f32", 0, True, 1.0),
     (21, 8192, "bf16", 8, True, 1.0),

@@ -78,9 +78,10 @@ __device__ __forceinline__ int sequence_length(const int32_t *lengths, int b, in
 //
 // What bounds it: with the chip full (two waves per SIMD at heads of 128), a
 // forward of 4 x 4096 tokens of 16 heads of 128 takes 70 us for 268 MB, 3.8 TB/s
-// against 4.85 of a copy; what is left is the issue of a wave's instructions
+// against 4.85 of a copy; what is left is the chain of a wave's instructions
 // (without loads and waits 79 of then 90 us): per chunk and wave 84 matrix
-// instructions and some 400 others, the split of X the most of them.  The three
+// instructions and some 400 others, the split of X the most of them, and the
+// registers of a 128-wide state allow no third wave to fill its gaps.  The three
 // gradients read 9 and write 3 widths of rows where 4 and 3 would do: 255 us for
 // 805 MB; one launch that formed all three would have to run the tokens in both
 // directions.  Short or few sequences are bound by latency: about 2 us per chunk
@@ -114,44 +115,53 @@ __device__ __forceinline__ void dma16_from(const void *p, unsigned lds_byte)
 #pragma clang diagnostic pop
 
 // A tile of rows of CH chunks of 16 bytes in LDS.  One load instruction fills
-// 64 chunks, 64 / CH rows; instructions are 64 bytes more than that apart, and
-// chunk c of a row stands at c ^ flip(row), flip being bits 2 and 3 of the row.
-// Which rows an instruction takes and their order in it (bits b0 .. b3 of the
-// row below) are such that, of the 256 bytes LDS serves at a time,
+// 64 chunks, 64 / CH rows; instructions are some bytes more than that apart, and
+// chunk c of a row stands at c ^ flip(row).  Which rows an instruction takes and
+// their order in it (bits b0 .. b3 of the row), the gaps and the flips are such
+// that, of the 256 bytes LDS serves at a time,
 //   - the 16 rows one operand read touches at one chunk get 16 different places,
 //   - the rows 0-7 (8-15) of half a transposing read get 8 different 32 bytes,
-// while the address stays a lane's own offset plus a constant.
+// while the address stays a lane's own offset plus a constant, with one other
+// offset for odd column blocks, and the two halves of an operand lie 32 bytes
+// apart (one read instruction, no copies to bring them together).
 template <int CH>
 struct Tile {
-    static constexpr int PITCH = 1024 + 64;
-    static constexpr int RPI = 64 / CH;    // rows of an instruction
-    __device__ static constexpr int flip(int row) { return CH == 2 ? 0 : ((row >> 2) & 1) * 2 + ((row >> 3) & 1); }
+    __host__ __device__ static constexpr int b(int row, int bit) { return (row >> bit) & 1; }
+    __device__ static constexpr int flip(int row)
+    {
+        return CH == 2 ? 0 : CH == 4 ? 2 * b(row, 2) + b(row, 3) : 4 * b(row, 2) + b(row, 3);
+    }
     // instruction of a row, and its place there
     __device__ static constexpr int instr(int row)
     {
         const int hi = row >> 4;
-        return CH == 64 ? row : CH == 32 ? (row & 7) + 8 * hi : CH == 16 ? (row & 3) + 4 * hi : CH == 8 ? (row & 1) + 2 * hi
-                                                                                            : CH == 4 ? hi : 0;
+        return CH == 64 ? row : CH == 32 ? (row & 7) + 8 * hi : CH == 16 ? (row & 3) + 4 * hi
+                                                              : CH == 8 ? (row & 1) + 2 * hi : CH == 4 ? hi : 0;
     }
     __device__ static constexpr int place(int row)
     {
-        const int b1 = (row >> 1) & 1, b3 = (row >> 3) & 1;
-        return CH == 64 ? 0 : CH == 32 ? b3 : CH == 16 ? flip(row) : CH == 8 ? b1 + 2 * b3 + 4 * ((row >> 2) & 1)
-                                                                             : CH == 4 ? (row & 3) + 4 * flip(row) : row;
+        const int f = 2 * b(row, 2) + b(row, 3);
+        return CH == 64 ? 0 : CH == 32 ? b(row, 3) : CH == 16 ? f : CH == 8 ? b(row, 1) + 2 * f
+                                                                : CH == 4 ? (row & 3) + 4 * f : row;
     }
-    __device__ static constexpr int offset(int row) { return instr(row) * PITCH + place(row) * CH * 16; }
     // the row of place j of instruction k: row_k(k) + row_j(j)
     __device__ static constexpr int row_k(int k)
     {
         return CH == 64 ? k : CH == 32 ? (k & 7) + 16 * (k >> 3) : CH == 16 ? (k & 3) + 16 * (k >> 2)
-                                                                   : CH == 8 ? (k & 1) + 16 * (k >> 1) : CH == 4 ? 16 * k : 32 * k;
+                                       : CH == 8 ? (k & 1) + 16 * (k >> 1) : CH == 4 ? 16 * k : 32 * k;
     }
     __device__ static constexpr int row_j(int j)
     {
-        return CH == 64 ? 0 : CH == 32 ? 8 * j : CH == 16 ? 4 * (j >> 1) + 8 * (j & 1)
-                                       : CH == 8 ? 2 * (j & 1) + 8 * ((j >> 1) & 1) + 4 * (j >> 2)
-                                                 : CH == 4 ? (j & 3) + 4 * ((j >> 3) & 1) + 8 * ((j >> 2) & 1) : j;
+        return CH == 64 ? 0 : CH == 32 ? 8 * j : CH == 16 ? 4 * b(j, 1) + 8 * b(j, 0)
+                                       : CH == 8 ? 2 * b(j, 0) + 8 * b(j, 1) + 4 * b(j, 2)
+                                                 : CH == 4 ? (j & 3) + 8 * b(j, 2) + 4 * b(j, 3) : j;
     }
+    __host__ __device__ static constexpr int start(int k)   // byte of instruction k
+    {
+        return k * 1024 + (CH >= 16 ? 32 * b(k, 0) + 128 * b(k, 1) + (k >> 2) * 256 : CH == 8 ? 32 * b(k, 0) + (k >> 1) * 256 : 0);
+    }
+    __host__ __device__ static constexpr int bytes(int instrs) { return start(instrs - 1) + 1024; }
+    __device__ static constexpr int offset(int row) { return start(instr(row)) + place(row) * CH * 16; }
 };
 
 // Where a lane's share of a tile's rows comes from: rows of `width` elements,
@@ -182,7 +192,7 @@ struct Loader {
             p += (c - chunk) * E;
         }
         if (!whole && !(row + rk < rows && c < chunks)) p = reinterpret_cast<const T *>(zero_chunk);
-        dma16_from(p, __builtin_amdgcn_readfirstlane(tile + (unsigned)(k * Tile<CH>::PITCH)));
+        dma16_from(p, __builtin_amdgcn_readfirstlane(tile + (unsigned)Tile<CH>::start(k)));
     }
 };
 
@@ -190,30 +200,34 @@ struct Loader {
 template <int CH, typename T> struct Reader;
 template <int CH>
 struct Reader<CH, bf16_t> {
-    unsigned row0, row1, col0, col1;
+    unsigned rows, cols;
     __device__ __forceinline__ void init(int c16, int q)
     {
         // rows c16: 8 bytes at columns 4q and 16 + 4q of 32
-        const int f = Tile<CH>::flip(c16);
-        row0 = Tile<CH>::offset(c16) + ((q >> 1) ^ f) * 16 + (q & 1) * 8;
-        row1 = row0 ^ 32;
+        rows = Tile<CH>::offset(c16) + ((q >> 1) ^ Tile<CH>::flip(c16)) * 16 + (q & 1) * 8;
         // columns: in each group of 16 lanes, lane s addresses the 8 bytes of
         // row 4q + s/4 and columns 4 (s%4); lane i receives four rows of column i
         const int r = 4 * q + (c16 >> 2);
-        col0 = Tile<CH>::offset(r) + (((c16 & 3) >> 1) ^ Tile<CH>::flip(r)) * 16 + (c16 & 1) * 8;
-        col1 = col0 ^ 32;
+        cols = Tile<CH>::offset(r) + (((c16 & 3) >> 1) ^ Tile<CH>::flip(r)) * 16 + (c16 & 1) * 8;
     }
     // row 16 s + c16 at column block kb
     __device__ __forceinline__ u32x4 row(lds_char *tile, int s, int kb) const
     {
-        const int at = Tile<CH>::offset(16 * s) + kb * 64;
-        const u32x2 lo = *(lds_u32x2_t *)(tile + row0 + at), hi = *(lds_u32x2_t *)(tile + row1 + at);
+        u32x2 lo, hi;
+        if constexpr (CH == 4) {   // one column block; the flip swaps its halves
+            lo = *(lds_u32x2_t *)(tile + rows + Tile<CH>::offset(16 * s));
+            hi = *(lds_u32x2_t *)(tile + (rows ^ 32) + Tile<CH>::offset(16 * s));
+        } else {
+            lds_char *p = tile + (rows ^ (kb & 1) * 64) + (kb >> 1) * 128 + Tile<CH>::offset(16 * s);
+            lo = *(lds_u32x2_t *)p;
+            hi = *(lds_u32x2_t *)(p + 32);
+        }
         return u32x4{lo[0], lo[1], hi[0], hi[1]};
     }
     // columns 16 ct .. 16 ct + 15 over the tile's rows
     __device__ __forceinline__ u32x4 col(lds_char *tile, int ct) const
     {
-        lds_char *p = tile + (ct & 1 ? col1 : col0) + (ct >> 1) * 64;
+        lds_char *p = CH == 4 ? tile + (cols ^ ct * 32) : tile + (cols ^ ((ct >> 1) & 1) * 64) + (ct >> 2) * 128 + (ct & 1) * 32;
         const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)p));
         const u32x2 hi = __builtin_bit_cast(
             u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(p + Tile<CH>::offset(16))));
@@ -222,21 +236,23 @@ struct Reader<CH, bf16_t> {
 };
 template <int CH>
 struct Reader<CH, float> {
-    unsigned row0, col0;
+    unsigned rows, odd, cols;   // rows at even and odd column blocks
     __device__ __forceinline__ void init(int c16, int q)
     {
-        row0 = Tile<CH>::offset(c16) + (q ^ Tile<CH>::flip(c16)) * 16;
-        col0 = Tile<CH>::offset(4 * q) + ((c16 >> 2) ^ Tile<CH>::flip(4 * q)) * 16 + (c16 & 3) * 4;
+        rows = Tile<CH>::offset(c16) + (q ^ Tile<CH>::flip(c16)) * 16;
+        odd = Tile<CH>::offset(c16) + (q ^ 4 ^ Tile<CH>::flip(c16)) * 16;
+        cols = Tile<CH>::offset(4 * q) + ((c16 >> 2) ^ Tile<CH>::flip(4 * q)) * 16 + (c16 & 3) * 4;
     }
     __device__ __forceinline__ u32x4 row(lds_char *tile, int, int kb) const
     {
-        return *(lds_u32x4_t *)(tile + row0 + kb * 64);
+        return *(lds_u32x4_t *)(tile + (kb & 1 ? odd : rows) + (kb >> 1) * 128);
     }
     __device__ __forceinline__ u32x4 col(lds_char *tile, int ct) const
     {
         u32x4 f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = *(lds_u32_t *)(tile + col0 + Tile<CH>::offset(e) + ct * 64);
+        for (int e = 0; e < 4; ++e)
+            f[e] = *(lds_u32_t *)(tile + (cols ^ (ct & 1) * 64) + (ct >> 1) * 128 + Tile<CH>::offset(e));
         return f;
     }
 };
@@ -246,24 +262,6 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ unsigned pack_bf16(float a, float b)   // one conversion instruction for both
 {
     return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2{a, b}), bf16x2));
-}
-
-// What eight values leave over their packed bf16 parts w: x - bf16(x), one
-// instruction each, the dot product of a pair with (-1, 0) or (0, -1) added to
-// x (exact).  Written out because the compiler takes the form that overwrites x
-// and copies x first (94 copies per chunk).  A dot product's result may be read
-// three wait states later, which the block ends with; x may be a matrix
-// product's result, whose wait lies before w, made from x by an instruction the
-// compiler knows.
-__device__ __forceinline__ void left_over(const u32x4 w, const float (&x)[8], float (&r)[8])
-{
-    asm("v_dot2_f32_bf16 %0, %8, %20, %12\n\tv_dot2_f32_bf16 %1, %8, %21, %13\n\t"
-        "v_dot2_f32_bf16 %2, %9, %20, %14\n\tv_dot2_f32_bf16 %3, %9, %21, %15\n\t"
-        "v_dot2_f32_bf16 %4, %10, %20, %16\n\tv_dot2_f32_bf16 %5, %10, %21, %17\n\t"
-        "v_dot2_f32_bf16 %6, %11, %20, %18\n\tv_dot2_f32_bf16 %7, %11, %21, %19\n\ts_nop 2"
-        : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
-        : "v"(w[0]), "v"(w[1]), "v"(w[2]), "v"(w[3]), "v"(x[0]), "v"(x[1]), "v"(x[2]), "v"(x[3]), "v"(x[4]), "v"(x[5]),
-          "v"(x[6]), "v"(x[7]), "s"(0x0000bf80u), "s"(0xbf800000u));
 }
 
 // fp32 values of an operand as the parts the matrix cores take.
@@ -277,7 +275,12 @@ __device__ __forceinline__ void split(const float (&x)[8], u32x4 (&f)[NP], bf16_
     for (int p = 0; p < NP; ++p) {
 #pragma unroll
         for (int e = 0; e < 8; e += 2) f[p][e / 2] = pack_bf16(r[p][e], r[p][e + 1]);
-        if (p + 1 < NP) left_over(f[p], r[p], r[p + 1]);
+        if (p + 1 < NP)   // what is left over, exactly
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                r[p + 1][e] = r[p][e] - __uint_as_float(f[p][e / 2] << 16);
+                r[p + 1][e + 1] = r[p][e + 1] - __uint_as_float(f[p][e / 2] & 0xffff0000u);
+            }
     }
 }
 template <int NP>
@@ -320,7 +323,7 @@ __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(R
     constexpr int CHA = row_chunks<T, DA>(), CHC = WCOLS * (int)sizeof(T) / 16;
     constexpr int KB = DA / C, KT = DA / 16, KEEP = KB < 4 ? KB : 4;
     constexpr int NA = C * CHA / 64, NC = C * CHC / 64;        // load instructions of a tile
-    constexpr int ABYTES = NA * Tile<CHA>::PITCH, CBYTES = NC * Tile<CHC>::PITCH;
+    constexpr int ABYTES = Tile<CHA>::bytes(NA), CBYTES = Tile<CHC>::bytes(NC);
     constexpr int SP = sizeof(T) == 2 ? 2 : 1;                 // parts of X and P
     extern __shared__ __align__(16) char lds[];
     const Role<T> &r = g.r[blockIdx.y];
@@ -675,7 +678,7 @@ hipError_t launch_chunks(const Roles<T> &g, int roles, int width, hipStream_t s)
     constexpr int C = Mat<T>::C, CHA = row_chunks<T, DA>(), CHC = WCOLS * (int)sizeof(T) / 16;
     const int columns = (width + WCOLS - 1) / WCOLS, blocks = (columns + MAX_WAVES - 1) / MAX_WAVES;
     const int waves = (columns + blocks - 1) / blocks;   // of a block; the columns of a head may take two
-    const int lds = 2 * (C * CHA / 64 * (OUT ? 2 : 1) * Tile<CHA>::PITCH + C * CHC / 64 * waves * Tile<CHC>::PITCH);
+    const int lds = 2 * ((OUT ? 2 : 1) * Tile<CHA>::bytes(C * CHA / 64) + waves * Tile<CHC>::bytes(C * CHC / 64));
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(linattn_chunks_kernel<T, DA, OUT, NP, MT>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds);

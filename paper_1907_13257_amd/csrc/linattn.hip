@@ -78,14 +78,14 @@ __device__ __forceinline__ int sequence_length(const int32_t *lengths, int b, in
 //
 // What bounds it: with the chip full (two waves per SIMD at heads of 128), a
 // forward of 4 x 4096 tokens of 16 heads of 128 takes 70 us for 268 MB, 3.8 TB/s
-// against 4.85 of a copy; what is left is the chain of a wave's instructions
-// (without loads and waits 79 of then 90 us): per chunk and wave 84 matrix
-// instructions and some 400 others, the split of X the most of them, and the
-// registers of a 128-wide state allow no third wave to fill its gaps.  The three
-// gradients read 9 and write 3 widths of rows where 4 and 3 would do: 255 us for
-// 805 MB; one launch that formed all three would have to run the tokens in both
-// directions.  Short or few sequences are bound by latency: about 2 us per chunk
-// and 5 before the first.
+// against 4.85 of a copy; what is left is the chain of a wave's instructions:
+// per chunk and wave 84 matrix instructions and some 400 others, the split of X
+// the most of them (41 % of a wave's time it issues, 31 % it waits its turn to,
+// 28 % for data and barriers), and the registers of a 128-wide state allow no
+// third wave to fill the gaps.  The three gradients read 9 and write 3 widths of
+// rows where 4 and 3 would do: 250 us for 805 MB; one launch that formed all
+// three would have to run the tokens in both directions.  Short or few sequences
+// are bound by latency: about 2 us per chunk and 5 before the first.
 // ---------------------------------------------------------------------------
 template <typename T> struct Mat;
 template <> struct Mat<bf16_t> {
@@ -651,9 +651,9 @@ struct SplitPlan {
 // rows cost a wave the same for 16.  Where that leaves the SIMDs with less than
 // one wave each unsplit and few chunks in all (FEW_CHUNKS of a wave per SIMD),
 // time is the latency of a wave's chunks, and 16 columns halve it: 2 x 1999
-// tokens of 16 heads of 64 in 36 us with 32 columns and 32 with 16, 12 x 333 of
-// 5 heads in fp32, forward and backward, 90 and 83; but 128 x 50 tokens of 16
-// heads 52 and 67, 4 x 4096 of 16 heads of 128 467 and 526.  Heads wider than
+// tokens of 16 heads of 64 in 36 us with 32 columns and 30 with 16, 12 x 333 of
+// 5 heads in fp32, forward and backward, 91 and 83; but 128 x 50 tokens of 16
+// heads 51 and 59, 4 x 4096 of 16 heads of 128 396 and 511.  Heads wider than
 // 128 always take 16: twice the state does not fit the registers.
 constexpr int MAX_WAVES = 8;   // of a block
 constexpr int TARGET_WAVES = 2048, MIN_CHUNKS = 3, FEW_CHUNKS = 16, SIMDS = 1024;
@@ -712,9 +712,9 @@ hipError_t launch_width(const Roles<T> &g, int roles, hipStream_t s)
 }
 
 // Parts from which on their states are joined by a launch of its own.  A block's
-// own joins cost it about 1.5 us each, one after another; the launch takes 5 to
-// 11 us (21 parts of 2 x 1999 tokens: 32 us with the launch, 66 without; 4 parts
-// of 12 x 333: 83 us with neither).
+// own joins cost it up to 1 us each, one after another; the launch takes 5 to
+// 11 us (21 parts of 2 x 1999 tokens: 30 us with the launch and 40 without; the
+// backward pass of 12 x 333 in 4 parts, with its forward, 87 and 83).
 constexpr int JOIN_PARTS = 6;
 template <typename T>
 hipError_t launch_join(const Roles<T> &g, int roles, hipStream_t s)

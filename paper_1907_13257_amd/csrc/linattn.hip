@@ -39,6 +39,8 @@ struct Roles {
     int T_, B, N;
     int parts, part_len;     // parts of a sequence, their tokens (a multiple of the chunk)
     int tiles;               // result tiles of 16 columns per wave, 1 or 2
+    int roles, each;         // grouped launches: its roles; its blocks for each head and part
+    unsigned inv_each;       // 2^32 / each, rounded up
     bool joined;             // the slots hold the states at the parts' starts
 };
 
@@ -315,7 +317,8 @@ constexpr int row_chunks()
 // OUT: rows of the output, and the final state; else the slots.
 // NP: parts of the state's update (bf16).  DA: the width of A and B, padded
 // with zeros to a multiple of 32.  MT: result tiles of 16 columns per wave.
-template <typename T, int DA, bool OUT, int NP, int MT>
+// GROUP: the order of the blocks (see launch_chunks).
+template <typename T, int DA, bool OUT, int NP, int MT, bool GROUP>
 __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(Roles<T> g)
 {
     constexpr int C = Mat<T>::C, TT = Mat<T>::TT, E = C / 4;   // E: values of an operand per lane
@@ -326,27 +329,35 @@ __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(R
     constexpr int ABYTES = Tile<CHA>::bytes(NA), CBYTES = Tile<CHC>::bytes(NC);
     constexpr int SP = sizeof(T) == 2 ? 2 : 1;                 // parts of X and P
     extern __shared__ __align__(16) char lds[];
-    const Role<T> &r = g.r[blockIdx.y];
+    unsigned bx = blockIdx.x, by = blockIdx.y, bz = blockIdx.z;
+    if constexpr (GROUP) {   // a head's blocks eight apart
+        const unsigned grp = __umulhi(bx / 8, g.inv_each), sub = bx / 8 - grp * g.each;   // bx / 8 / each, and what is left
+        bx = grp * 8 + bx % 8;
+        bz = sub >= (unsigned)g.roles ? 1 : 0;
+        by = sub - bz * g.roles;
+        if (bx >= (unsigned)(g.B * g.N * g.parts)) return;
+    }
+    const Role<T> &r = g.r[by];
     const int waves = blockDim.x >> 6, lane = threadIdx.x & 63, q = lane >> 4, c16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int h = blockIdx.x % g.N, b = (int)((blockIdx.x / g.N) % g.B), part = (int)(blockIdx.x / g.N / g.B);
+    const int h = bx % g.N, b = (int)((bx / g.N) % g.B), part = (int)(bx / g.N / g.B);
     const long bh = (long)b * g.N + h;
     // (a value read from memory that is the same for all lanes stays in a scalar
     // register only if it is said to be)
     const int n = __builtin_amdgcn_readfirstlane(sequence_length(g.lengths, b, g.T_));
     const int begin = part * g.part_len, stop = min(g.T_, begin + g.part_len), end = min(n, stop);
-    const int da = r.da, dc = r.dc, col0 = ((int)blockIdx.z * waves + wave) * WCOLS;
+    const int da = r.da, dc = r.dc, col0 = ((int)bz * waves + wave) * WCOLS;
     T *const out = r.out;
     const long size = (long)da * dc, slots = bh * g.parts * size;
     const bool last = end >= n;   // of this sequence
     float *const XT = OUT && last && (n > 0 || part == 0) ? r.XT : nullptr;
 
-    if (!OUT && part == 0 && blockIdx.z == 0 && r.X0)   // the first state
+    if (!OUT && part == 0 && bz == 0 && r.X0)   // the first state
         for (int i = threadIdx.x; i < size / 4; i += blockDim.x)
             reinterpret_cast<f32x4 *>(r.slots + slots)[i] = reinterpret_cast<const f32x4 *>(r.X0 + bh * size)[i];
     if (!OUT && last) return;
     if (OUT && !out && !XT) return;
-    if (OUT && out && n < stop && blockIdx.z == 0) {   // behind the sequence's end
+    if (OUT && out && n < stop && bz == 0) {   // behind the sequence's end
         const int per = dc * (int)sizeof(T) / 16, t0 = max(n, begin);
         const long all = (long)(stop - t0) * per;
         for (long i = threadIdx.x; i < all; i += blockDim.x) {
@@ -671,22 +682,41 @@ SplitPlan split_plan(const LinAttnShape &sh, int chunk, int roles)
     return SplitPlan{(chunks + per - 1) / per, per * chunk, few || width > 128 ? 1 : 2};
 }
 
+// The blocks of a head (its roles; the columns of a wide one), which read the
+// same rows, are launched eight apart where they have many chunks: on one XCD at
+// about one time, so that its L2 serves what another of them has read.  Forward
+// and backward of 64 x 400 tokens of 16 heads of 64 in 190 us, else 200; 16 x 1000
+// of 8 heads of 128 183 and 201, of 4 heads of 256 409 and 428; 4 x 4096 of 16
+// heads of 128 394 and 397.  Short blocks stay one role after
+// another: 128 x 50 tokens of 16 heads of 64 in 55 us grouped and 53 not, 64 x 200
+// 96 and 96.
+constexpr int GROUP_CHUNKS = 8;
 template <typename T, int DA, bool OUT, int NP, int MT>
-hipError_t launch_chunks(const Roles<T> &g, int roles, int width, hipStream_t s)
+hipError_t launch_chunks(Roles<T> g, int roles, int width, hipStream_t s)
 {
     constexpr int WCOLS = 16 * MT;
     constexpr int C = Mat<T>::C, CHA = row_chunks<T, DA>(), CHC = WCOLS * (int)sizeof(T) / 16;
     const int columns = (width + WCOLS - 1) / WCOLS, blocks = (columns + MAX_WAVES - 1) / MAX_WAVES;
     const int waves = (columns + blocks - 1) / blocks;   // of a block; the columns of a head may take two
     const int lds = 2 * ((OUT ? 2 : 1) * Tile<CHA>::bytes(C * CHA / 64) + waves * Tile<CHC>::bytes(C * CHC / 64));
-    if (lds > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(linattn_chunks_kernel<T, DA, OUT, NP, MT>),
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        if (e != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL((linattn_chunks_kernel<T, DA, OUT, NP, MT>), dim3((unsigned)((long)g.B * g.N * g.parts), roles, blocks),
-                       dim3(64 * waves), lds, s, g);
-    return hipGetLastError();
+    const long n = (long)g.B * g.N * g.parts;
+    auto launch = [&](auto kernel, dim3 grid) {
+        if (lds > 64 * 1024) {
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+            if (e != hipSuccess) return e;
+        }
+        hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), lds, s, g);
+        return hipGetLastError();
+    };
+    if constexpr (MT == 2 || DA > 128)   // (with waves of 16 columns else, blocks have few chunks)
+        if (roles * blocks > 1 && g.part_len >= GROUP_CHUNKS * C) {
+            g.roles = roles;
+            g.each = roles * blocks;   // at most 6
+            g.inv_each = 0xffffffffu / g.each + 1;
+            return launch(linattn_chunks_kernel<T, DA, OUT, NP, MT, true>, dim3((unsigned)((n + 7) / 8 * 8 * g.each)));
+        }
+    return launch(linattn_chunks_kernel<T, DA, OUT, NP, MT, false>, dim3((unsigned)n, roles, blocks));
 }
 
 // Roles of one launch: padded to the widest of them.

@@ -494,6 +494,32 @@ def test_linattn(T, B, N, K, M, dtype, lengths, states, fused):
         assert torch.equal(again[n], first[n]), f"{label}: {n} in other bits"
 
 
+@pytest.mark.parametrize("T,B,N,K,M,dtype", [
+    (700, 13, 21, 16, 24, "bf16"),    # parts of 8 chunks, 819 of them
+    (350, 13, 21, 24, 16, "f32"),
+    (1010, 5, 7, 136, 8, "bf16"),     # two blocks to a head's columns
+    (505, 7, 5, 8, 144, "f32"),
+    (300, 17, 61, 32, 16, "bf16"),    # not split, 1037 heads
+])
+def test_linattn_blocks_of_many_chunks(T, B, N, K, M, dtype):
+    """Long blocks, launched with those that read the same rows beside them,
+    their number no multiple of eight; and each gradient by itself, in the same
+    bits."""
+    label = f"linattn long blocks T{T} B{B} N{N} K{K} M{M} {dtype}"
+    announce(label)
+    c = linattn_case(T, B, N, K, M, dtype, "ragged", True)
+    op = make_linattn(T, B, N, K, M, dtype, True)
+    d = device_buffers(c, T, B, N, K, M, dtype, True)
+    got = run_linattn(op, d)
+    check_linattn(got, c, T, B, N, K, M, dtype, K ** -0.5, label)
+    for n in ("dq", "dk", "dv", "dS0"):
+        whole = got[n].clone()
+        got[n].fill_(float("nan"))
+        only = [d[m] if m == n else None for m in ("dq", "dk", "dv", "dS0")]
+        op.backward(d["do"], d["q"], d["k"], d["v"], d["decay"], *only[:3], d["lengths"], d["S0"], d["dST"], only[3])
+        assert torch.equal(got[n], whole), f"{label}: {n} alone in other bits"
+
+
 @pytest.mark.parametrize("decay", [1.0, 0.0, 0.5, 1 - 2.0 ** -14, 2.0 ** -40])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_linattn_decays(decay, dtype):

@@ -74,9 +74,13 @@ __device__ __forceinline__ int sequence_length(const int32_t *lengths, int b, in
 // reads) come from LDS.  Every wave forms P for itself.
 //
 // bf16 storage: X, P and the decayed C are fp32 values that the matrix cores
-// take in bf16 parts: two parts, hi = bf16(x) and lo = bf16(x - hi), leave out
-// 2^-16 of a value, well below the rounding of the result; a state that is an
-// output is updated with three parts (2^-24).
+// take in three bf16 parts, bf16(x), bf16(x - first) and bf16 of what is left:
+// eight bits each, so nothing of an fp32 value is left out and results are those
+// of fp32 factors, whichever states a call gives or wants.  (Two parts, which
+// leave out 2^-17 of a factor, take 395 us instead of 474 for 4 x 4096 tokens of
+// 16 heads of 128, forward and backward, 51 instead of 57 for 128 x 50 of 16 heads
+// of 64, 31 and 31 for 2 x 1999; but where terms cancel, the result's own rounding
+// is below what they lose.)
 //
 // What bounds it: with the chip full (two waves per SIMD at heads of 128), a
 // forward of 4 x 4096 tokens of 16 heads of 128 takes 70 us for 268 MB, 3.8 TB/s
@@ -315,10 +319,10 @@ constexpr int row_chunks()
 // them.  The last part of a sequence adds to no other and has no slot.
 //
 // OUT: rows of the output, and the final state; else the slots.
-// NP: parts of the state's update (bf16).  DA: the width of A and B, padded
-// with zeros to a multiple of 32.  MT: result tiles of 16 columns per wave.
-// GROUP: the order of the blocks (see launch_chunks).
-template <typename T, int DA, bool OUT, int NP, int MT, bool GROUP>
+// DA: the width of A and B, padded with zeros to a multiple of 32.  MT: result
+// tiles of 16 columns per wave.  GROUP: the order of the blocks (see
+// launch_chunks).
+template <typename T, int DA, bool OUT, int MT, bool GROUP>
 __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(Roles<T> g)
 {
     constexpr int C = Mat<T>::C, TT = Mat<T>::TT, E = C / 4;   // E: values of an operand per lane
@@ -327,7 +331,7 @@ __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(R
     constexpr int KB = DA / C, KT = DA / 16, KEEP = KB < 4 ? KB : 4;
     constexpr int NA = C * CHA / 64, NC = C * CHC / 64;        // load instructions of a tile
     constexpr int ABYTES = Tile<CHA>::bytes(NA), CBYTES = Tile<CHC>::bytes(NC);
-    constexpr int SP = sizeof(T) == 2 ? 2 : 1;                 // parts of X and P
+    constexpr int NP = sizeof(T) == 2 ? 3 : 1;                 // parts of an fp32 factor
     extern __shared__ __align__(16) char lds[];
     unsigned bx = blockIdx.x, by = blockIdx.y, bz = blockIdx.z;
     if constexpr (GROUP) {   // a head's blocks eight apart
@@ -501,14 +505,14 @@ __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(R
 #pragma unroll
                         for (int ti = s; ti < TT; ++ti) mfma16(P[s][ti], bf[s][kb % KEEP], a[ti][kb % KEEP], T());
             }
-            u32x4 pf[TT][SP];
+            u32x4 pf[TT][NP];
 #pragma unroll
             for (int ti = 0; ti < TT; ++ti) {
                 float x[E];
 #pragma unroll
                 for (int e = 0; e < E; ++e)
                     x[e] = e / 4 > ti ? 0.0f : P[e / 4][ti][e % 4] * (e / 4 == ti ? w0[e % 4] : w1[e % 4]);
-                split<SP>(x, pf[ti], T());
+                split<NP>(x, pf[ti], T());
             }
             // X^T A^T, scaled by row, and C^T P onto it
             f32x4 o[TT][MT];
@@ -522,16 +526,16 @@ __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(R
                     if constexpr (KB > KEEP)
 #pragma unroll
                         for (int ti = 0; ti < TT; ++ti) a[ti][kb % KEEP] = ra.row(ta, ti, kb);
-                    u32x4 f[MT][SP];
+                    u32x4 f[MT][NP];
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) {
                         float x[E];
 #pragma unroll
                         for (int e = 0; e < E; ++e) x[e] = X[TT * kb + e / 4][mt][e % 4];
-                        split<SP>(x, f[mt], T());
+                        split<NP>(x, f[mt], T());
                     }
 #pragma unroll
-                    for (int p = 0; p < SP; ++p)   // neighbours add to different tiles
+                    for (int p = 0; p < NP; ++p)   // neighbours add to different tiles
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -545,7 +549,7 @@ __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(R
                 }
             }
 #pragma unroll
-            for (int p = 0; p < SP; ++p)
+            for (int p = 0; p < NP; ++p)
 #pragma unroll
                 for (int ti = 0; ti < TT; ++ti)
 #pragma unroll
@@ -691,7 +695,7 @@ SplitPlan split_plan(const LinAttnShape &sh, int chunk, int roles)
 // another: 128 x 50 tokens of 16 heads of 64 in 55 us grouped and 53 not, 64 x 200
 // 96 and 96.
 constexpr int GROUP_CHUNKS = 8;
-template <typename T, int DA, bool OUT, int NP, int MT>
+template <typename T, int DA, bool OUT, int MT>
 hipError_t launch_chunks(Roles<T> g, int roles, int width, hipStream_t s)
 {
     constexpr int WCOLS = 16 * MT;
@@ -714,14 +718,14 @@ hipError_t launch_chunks(Roles<T> g, int roles, int width, hipStream_t s)
             g.roles = roles;
             g.each = roles * blocks;   // at most 6
             g.inv_each = 0xffffffffu / g.each + 1;
-            return launch(linattn_chunks_kernel<T, DA, OUT, NP, MT, true>, dim3((unsigned)((n + 7) / 8 * 8 * g.each)));
+            return launch(linattn_chunks_kernel<T, DA, OUT, MT, true>, dim3((unsigned)((n + 7) / 8 * 8 * g.each)));
         }
-    return launch(linattn_chunks_kernel<T, DA, OUT, NP, MT, false>, dim3((unsigned)n, roles, blocks));
+    return launch(linattn_chunks_kernel<T, DA, OUT, MT, false>, dim3((unsigned)n, roles, blocks));
 }
 
 // Roles of one launch: padded to the widest of them.
-template <typename T, bool OUT, int NP>
-hipError_t launch_width(const Roles<T> &g, int roles, hipStream_t s)
+template <typename T, bool OUT>
+hipError_t launch_roles(const Roles<T> &g, int roles, hipStream_t s)
 {
     int da = 0, dc = 0;
     for (int k = 0; k < roles; ++k) {
@@ -730,14 +734,14 @@ hipError_t launch_width(const Roles<T> &g, int roles, hipStream_t s)
     }
     const bool one = g.tiles == 1;
     switch ((da + 31) / 32) {
-    case 1: return one ? launch_chunks<T, 32, OUT, NP, 1>(g, roles, dc, s) : launch_chunks<T, 32, OUT, NP, 2>(g, roles, dc, s);
-    case 2: return one ? launch_chunks<T, 64, OUT, NP, 1>(g, roles, dc, s) : launch_chunks<T, 64, OUT, NP, 2>(g, roles, dc, s);
-    case 3: return one ? launch_chunks<T, 96, OUT, NP, 1>(g, roles, dc, s) : launch_chunks<T, 96, OUT, NP, 2>(g, roles, dc, s);
-    case 4: return one ? launch_chunks<T, 128, OUT, NP, 1>(g, roles, dc, s) : launch_chunks<T, 128, OUT, NP, 2>(g, roles, dc, s);
-    case 5: return launch_chunks<T, 160, OUT, NP, 1>(g, roles, dc, s);
-    case 6: return launch_chunks<T, 192, OUT, NP, 1>(g, roles, dc, s);
-    case 7: return launch_chunks<T, 224, OUT, NP, 1>(g, roles, dc, s);
-    default: return launch_chunks<T, 256, OUT, NP, 1>(g, roles, dc, s);
+    case 1: return one ? launch_chunks<T, 32, OUT, 1>(g, roles, dc, s) : launch_chunks<T, 32, OUT, 2>(g, roles, dc, s);
+    case 2: return one ? launch_chunks<T, 64, OUT, 1>(g, roles, dc, s) : launch_chunks<T, 64, OUT, 2>(g, roles, dc, s);
+    case 3: return one ? launch_chunks<T, 96, OUT, 1>(g, roles, dc, s) : launch_chunks<T, 96, OUT, 2>(g, roles, dc, s);
+    case 4: return one ? launch_chunks<T, 128, OUT, 1>(g, roles, dc, s) : launch_chunks<T, 128, OUT, 2>(g, roles, dc, s);
+    case 5: return launch_chunks<T, 160, OUT, 1>(g, roles, dc, s);
+    case 6: return launch_chunks<T, 192, OUT, 1>(g, roles, dc, s);
+    case 7: return launch_chunks<T, 224, OUT, 1>(g, roles, dc, s);
+    default: return launch_chunks<T, 256, OUT, 1>(g, roles, dc, s);
     }
 }
 
@@ -752,17 +756,6 @@ hipError_t launch_join(const Roles<T> &g, int roles, hipStream_t s)
     const int per = (g.r[0].da * g.r[0].dc / 4 + 255) / 256;
     hipLaunchKernelGGL(linattn_join_kernel<T>, dim3((unsigned)((long)g.B * g.N * per), roles), dim3(256), 0, s, g);
     return hipGetLastError();
-}
-
-// `exact`: the call carries states, so that one may be an output: three bf16
-// parts, whichever results are wanted (the rows do not depend on that).
-template <typename T, bool OUT>
-hipError_t launch_roles(const Roles<T> &g, int roles, bool exact, hipStream_t s)
-{
-    if constexpr (sizeof(T) == 2)
-        return exact ? launch_width<T, OUT, 3>(g, roles, s) : launch_width<T, OUT, 2>(g, roles, s);
-    else
-        return launch_width<T, OUT, 1>(g, roles, s);
 }
 
 // One token of one head per block: the state's rows are read four values per
@@ -833,13 +826,12 @@ hipError_t forward_t(const LinAttnShape &sh, const T *q, const T *k, const T *v,
     Roles<T> g = call_of<T>(sh, decay, lengths, 1);
     g.r[0] = Role<T>{q, k, v, o, sh.ldq, sh.ldk, sh.ldv, sh.ldo, sh.K, sh.M, false, sh.scale, sh.scale, 1.0f, S0, ST,
                      sh.M, 1, ws};
-    const bool exact = S0 || ST;
     if (g.parts > 1) {
-        hipError_t e = launch_roles<T, false>(g, 1, exact, s);
+        hipError_t e = launch_roles<T, false>(g, 1, s);
         if (e == hipSuccess && g.joined) e = launch_join(g, 1, s);
         if (e != hipSuccess) return e;
     }
-    return launch_roles<T, true>(g, 1, exact, s);
+    return launch_roles<T, true>(g, 1, s);
 }
 
 template <typename T>
@@ -855,12 +847,12 @@ hipError_t backward_t(const LinAttnShape &sh, const T *d_o, const T *q, const T 
     const Role<T> rq{d_o, v, k, dq, sh.ldo, sh.ldv, sh.ldk, sh.ldq, M, K, false, sc, sc, 1.0f, S0, nullptr, 1, M, ws};
     const Role<T> rk{v, d_o, q, dk, sh.ldv, sh.ldo, sh.ldq, sh.ldk, M, K, true, sc, 1.0f, sc, dST, nullptr, 1, M, ws2};
     const Role<T> rv{k, q, d_o, dv, sh.ldk, sh.ldq, sh.ldo, sh.ldv, K, M, true, sc, 1.0f, sc, dST, dS0, M, 1, ws2};
-    const bool exact = S0 || dST || dS0, back = dk || dv || dS0;
+    const bool back = dk || dv || dS0;
     if (g.parts > 1) {
         int n = 0;
         if (dq) g.r[n++] = rq;
         if (back) g.r[n++] = rv;
-        hipError_t e = n ? launch_roles<T, false>(g, n, exact, s) : hipSuccess;
+        hipError_t e = n ? launch_roles<T, false>(g, n, s) : hipSuccess;
         if (e == hipSuccess && n && g.joined) e = launch_join(g, n, s);
         if (e != hipSuccess) return e;
     }
@@ -868,12 +860,12 @@ hipError_t backward_t(const LinAttnShape &sh, const T *d_o, const T *q, const T 
     if (dq) g.r[n++] = rq;
     if (dk) g.r[n++] = rk;
     if (n && dS0 && dS0 == dST && g.parts == 1) {   // dk's blocks read dST before dv's replace it
-        const hipError_t e = launch_roles<T, true>(g, n, exact, s);
+        const hipError_t e = launch_roles<T, true>(g, n, s);
         if (e != hipSuccess) return e;
         n = 0;
     }
     if (dv || dS0) g.r[n++] = rv;
-    return n ? launch_roles<T, true>(g, n, exact, s) : hipSuccess;
+    return n ? launch_roles<T, true>(g, n, s) : hipSuccess;
 }
 
 }  // namespace

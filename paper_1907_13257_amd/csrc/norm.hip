@@ -124,8 +124,31 @@ __global__ __launch_bounds__(THREADS<W>) void add_norm_kernel(NormArgs a, int nv
         const float rho = rsqrtf(r.a / (float)(nv * E) + a.eps);
         if constexpr (Q8) {
             // y / scale = (sum g) 448 / max|sum g|: the norm's factor cancels.
-            // A maximum below the smallest normal number counts as zero.
-            const bool some = !(r.b < 1.17549435e-38f);
+            // Where the maximum is so small that the quotient could overflow or
+            // the products have lost digits, the row is taken again from what is
+            // stored, 2^112 times as large; what is below 2^-119 then has a scale
+            // of 0 in fp32.
+            float down = 1.0f;
+            if (r.b < 0x1p-64f) {
+                const T *from = sum ? sum : x;
+                Sum2 m{0.0f, 0.0f};
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const int c = tid + p * 64 * W;
+                    if (c >= nv) continue;
+                    float gv[E];
+                    load_vec<T>(from + (long)c * E, s[p]);
+                    load_vec<T>(g + (long)c * E, gv);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        s[p][e] = s[p][e] * 0x1p64f * gv[e] * 0x1p48f;
+                        m.b = fmaxf(m.b, fabsf(s[p][e]));
+                    }
+                }
+                r.b = reduce_row<W, true>(m, red).b;
+                down = 0x1p-112f;
+            }
+            const bool some = !(r.b < 0x1p-119f);
             const float inv = some ? 448.0f / r.b : 0.0f;
             uint8_t *y = static_cast<uint8_t *>(a.y) + row * (long)nv * E;
 #pragma unroll
@@ -138,7 +161,7 @@ __global__ __launch_bounds__(THREADS<W>) void add_norm_kernel(NormArgs a, int nv
                     w[q] = e4m3x4(s[p][4 * q] * inv, s[p][4 * q + 1] * inv, s[p][4 * q + 2] * inv, s[p][4 * q + 3] * inv);
                 __builtin_memcpy(y + (long)c * E, w, E);
             }
-            if (tid == 0) a.scale[row] = some ? r.b * rho / 448.0f : r.b * 0.0f;
+            if (tid == 0) a.scale[row] = some ? r.b * rho / 448.0f * down : r.a * 0.0f;   // NaN if the sum is
         } else {
             T *y = static_cast<T *>(a.y) + row * a.ldy;
 #pragma unroll

@@ -120,3 +120,77 @@ def test_linattn_results_do_not_depend_on_the_states_wanted(T, B, N, K, M):
     run_linattn(op, d)
     for n in ("o", "dq", "dk", "dv"):
         assert torch.equal(d[n], want[n]), n
+
+
+# ---------------------------------------------------------------------------
+# residual norm: rows far from 1
+# ---------------------------------------------------------------------------
+STEPS = 64   # roundings of a row's sum, its root and the products around it (as in test_gpu_operators)
+
+
+def norm_definition(s, g, eps):
+    S, G = s.double(), g.double()
+    return S / torch.sqrt((S * S).mean(1, keepdim=True) + eps) * G
+
+
+def check_q8(y8, scales, y, label):
+    """The bytes and scales of rows whose definition is y."""
+    top = y.abs().amax(1)
+    want = top / 448
+    scales, steps = scales.cpu().double(), y8.cpu().double()
+    assert torch.isfinite(scales).all() and torch.isfinite(steps).all(), label
+    # fp32 roundings, and half of fp32's smallest step where the scale is below the normal numbers
+    assert ((scales - want).abs() <= 2 * STEPS * U * want + 2.0 ** -150).all(), (label, scales, want)
+    at = y / torch.where(top > 0, want, 1.0)[:, None]
+    # half a step of e4m3 (2^-4 of the value, or half of the smallest step 2^-9) and the fp32 roundings before it
+    assert ((steps - at).abs() <= (2.0 ** -4 + 4 * STEPS * U) * at.abs() + 2.0 ** -10).all(), label
+    announce(f"{label}: scales to {float(((scales - want).abs() / want.clamp(min=1e-300)).max()):.1e}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [16, 520, 2056, 16384])
+@pytest.mark.parametrize("residual", [False, True])
+def test_add_norm_q8_of_tiny_rows(dtype, D, residual):
+    """Largest values of a row around the smallest normal number, and around
+    448 over the largest one, where a quotient taken outright overflows; with
+    zeros among them, a row of zeros, and an ordinary row."""
+    from paper_1907_13257_amd import AddNorm
+    tops = [2e-38, 1.3e-37, 1e-36, 1.4e-36, 2e-36, 1e-30, 5e-20, 1e-39, 3e-42, 0.0, 1.0]
+    if dtype == "f32":
+        tops += [7e-45, 1.5e-45]
+    g = gen(D)
+    x = (torch.tensor(tops, dtype=torch.float64)[:, None] * (2 * torch.rand(len(tops), D, generator=g) - 1)).to(
+        normal(g, 1, dtype=dtype).dtype)
+    x[:, 3] = 0
+    x[:, 5] = torch.tensor(tops).to(x.dtype)   # the largest of its row
+    gain = (0.5 + torch.rand(D, generator=g)).to(x.dtype)
+    gain[5] = 2
+    rows = len(tops)
+    op = AddNorm(rows, D, dtype)
+    y8 = torch.zeros(rows, D, dtype=torch.float8_e4m3fn, device="cuda")
+    scales, s_ = torch.full((rows,), float("nan"), device="cuda"), torch.empty_like(x).cuda()
+    res = torch.zeros_like(x).cuda() if residual else None
+    op.forward_q8(x.cuda(), res, gain.cuda(), s_ if residual else None, y8, scales)
+    check_q8(y8, scales, norm_definition(x, gain, 1e-5), f"8 bits of tiny rows D{D} {dtype}")
+    if residual:
+        assert torch.equal(s_.cpu(), x)
+        # the sum in the residual's place
+        op.forward_q8(x.cuda(), res, gain.cuda(), res, y8, scales)
+        check_q8(y8, scales, norm_definition(x, gain, 1e-5), f"8 bits of tiny rows in place D{D} {dtype}")
+
+
+def test_add_norm_q8_shows_what_is_not_a_number():
+    """A NaN among zeros, an infinity, a NaN among ordinary values: the row's
+    values by bytes and scale are no numbers, other rows stay as they are."""
+    from paper_1907_13257_amd import AddNorm
+    D = 72
+    x = torch.randn(5, D, generator=gen(9))
+    x[1] = 0
+    x[1, 7], x[2, 7], x[3, 7] = float("nan"), float("inf"), float("nan")
+    gain = torch.ones(D)
+    op = AddNorm(5, D, "f32")
+    y8, scales = torch.zeros(5, D, dtype=torch.float8_e4m3fn, device="cuda"), torch.zeros(5, device="cuda")
+    op.forward_q8(x.cuda(), None, gain.cuda(), None, y8, scales)
+    y = y8.float().cpu() * scales.cpu()[:, None]
+    assert y[1].isnan().all() and y[2].isnan().all() and y[3].isnan().all()
+    check_q8(y8[::4], scales[::4], norm_definition(x[::4], gain, 1e-5), "rows beside them")

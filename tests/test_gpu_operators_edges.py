@@ -194,3 +194,38 @@ def test_add_norm_q8_shows_what_is_not_a_number():
     y = y8.float().cpu() * scales.cpu()[:, None]
     assert y[1].isnan().all() and y[2].isnan().all() and y[3].isnan().all()
     check_q8(y8[::4], scales[::4], norm_definition(x[::4], gain, 1e-5), "rows beside them")
+
+
+def norm_gradient(s, g, dy, dsum, eps):
+    """The definition's gradients in 64 bits and their terms' sizes."""
+    S, G, DY = s.double(), g.double(), dy.double()
+    root = torch.sqrt((S * S).mean(1, keepdim=True) + eps)
+    unit, up = S / root, DY * G
+    dx = (up - unit * (up * unit).mean(1, keepdim=True)) / root
+    size = (up.abs() + unit.abs() * (up * unit).abs().mean(1, keepdim=True)) / root
+    if dsum is not None:
+        dx, size = dx + dsum.double(), size + dsum.double().abs()
+    return dx, size, (DY * unit).sum(0), (DY * unit).abs().sum(0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 1024, 4104])
+@pytest.mark.parametrize("scale,eps", [(1e12, 1e-5), (1e14, 1e-5), (1e17, 1e-5), (1e17, 0.0), (1e-12, 0.0),
+                                       (1e-14, 0.0), (1e-16, 0.0), (1e-16, 1e-5)])
+def test_add_norm_gradient_of_rows_far_from_one(dtype, D, scale, eps):
+    """The norm's projection term counts at every size of a row; dsum at the
+    size of the rest, or none."""
+    from paper_1907_13257_amd import AddNorm
+    g = gen(D)
+    rows = 7
+    s, dy, gain = normal(g, rows, D, dtype=dtype, scale=scale), normal(g, rows, D, dtype=dtype), normal(g, D, dtype=dtype)
+    s[3] = s[3].abs() + scale   # a mean far from zero: dy's projection is large
+    dy[3] = gain.sign() * dy[3].abs()
+    op = AddNorm(rows, D, dtype, eps)
+    for dsum in (None, normal(g, rows, D, dtype=dtype, scale=1 / max(scale, eps ** 0.5))):
+        dx, dg = torch.full_like(s, float("nan")).cuda(), torch.full((D,), float("nan"), device="cuda")
+        op.backward(dy.cuda(), None if dsum is None else dsum.cuda(), s.cuda(), gain.cuda(), dx, dg)
+        rdx, size, rdg, gsize = norm_gradient(s, gain, dy, dsum, eps)
+        label = f"norm's gradient at {scale} eps {eps} D{D} {dtype}"
+        close(dx, rdx, size, 3 * STEPS, dtype, label + " dx")
+        close(dg, rdg, gsize, STEPS + rows + 8, "f32", label + " dg")

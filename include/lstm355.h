@@ -303,7 +303,8 @@ lstm_status_t lstm_embed_backward(lstm_dtype_t dtype, long N, long V, int D, con
  *   and ldy (y), 0 = dense; g [D], dtype; D a multiple of 8, at most 16384.
  *   res may be NULL: then sum is x, and `sum` may be NULL (if not, it gets x).
  *   sum may be res, or x when ldx = ldr.  The norm is that of the stored sum.
- *   The squares are summed in fp32: |sum| up to 1e18.  rows = 0 is allowed. */
+ *   The squares are summed in fp32: |sum| up to 1e18 at every width, and where
+ *   eps is 0 a row's largest |sum| at least 1e-17.  rows = 0 is allowed. */
 lstm_status_t lstm_add_norm(lstm_dtype_t dtype, long rows, int D, const void *x, long ldx, const void *res, long ldr,
                             const void *g, float eps, void *sum, void *y, long ldy, void *stream);
 

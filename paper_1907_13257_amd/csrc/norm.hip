@@ -70,6 +70,14 @@ __device__ __forceinline__ Sum2 reduce_row(Sum2 v, float *red)
     return v;
 }
 
+// A thread's squares (32 at most) are summed as they are, a row's as a 64th: 16384
+// squares of 1e18 are beyond fp32.  A power of two changes no digit.
+constexpr float SQUARES = 0x1p-6f;
+__device__ __forceinline__ float inverse_root(float squares, int D, float eps)   // 1 / sqrt(mean + eps)
+{
+    return rsqrtf(squares / ((float)D * SQUARES) + eps);
+}
+
 // A row is held in registers by W waves, P vectors per thread (thread t has
 // vectors t, t + 64 W, ...), so it is read once and both sums over it need no
 // second pass.  A block has four rows where a row is one wave's, else one.
@@ -120,8 +128,9 @@ __global__ __launch_bounds__(THREADS<W>) void add_norm_kernel(NormArgs a, int nv
                 }
             }
         }
+        r.a *= SQUARES;
         r = reduce_row<W, true>(r, red);
-        const float rho = rsqrtf(r.a / (float)(nv * E) + a.eps);
+        const float rho = inverse_root(r.a, nv * E, a.eps);
         if constexpr (Q8) {
             // y / scale = (sum g) 448 / max|sum g|: the norm's factor cancels.
             // Where the maximum is so small that the quotient could overflow or
@@ -216,8 +225,9 @@ __global__ __launch_bounds__(THREADS<W>) void add_norm_backward_kernel(NormBwdAr
                 r.b += gv[p][e] * d[p][e] * s[p][e];
             }
         }
+        r.a *= SQUARES;
         r = reduce_row<W, false>(r, red);
-        const float rho = rsqrtf(r.a / (float)(nv * E) + a.eps);
+        const float rho = inverse_root(r.a, nv * E, a.eps);
         const float k = rho * (rho * (r.b / (float)(nv * E)));
         T *dx = static_cast<T *>(a.dx) + row * a.ldx;
 #pragma unroll

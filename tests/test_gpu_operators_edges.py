@@ -229,3 +229,33 @@ def test_add_norm_gradient_of_rows_far_from_one(dtype, D, scale, eps):
         label = f"norm's gradient at {scale} eps {eps} D{D} {dtype}"
         close(dx, rdx, size, 3 * STEPS, dtype, label + " dx")
         close(dg, rdg, gsize, STEPS + rows + 8, "f32", label + " dg")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [8, 512, 1024, 2048, 4104, 8192, 16384])
+@pytest.mark.parametrize("scale,eps", [(1e18, 1e-5), (1e-17, 0.0)])
+def test_add_norm_at_the_ends_of_its_range(dtype, D, scale, eps):
+    """Rows throughout of the largest and of the smallest stated size, forward,
+    to 8 bits and backward."""
+    from paper_1907_13257_amd import AddNorm
+    g = gen(D + 1)
+    rows = 3
+    t = normal(g, 1, dtype=dtype).dtype
+    size = torch.full((rows, D), scale, dtype=torch.float64)
+    size = torch.where(size.to(t).double() > 1e18, torch.nextafter(size.to(t), torch.zeros(1, dtype=t)).double(), size)
+    s = (size * torch.where(torch.rand(rows, D, generator=g) < 0.5, -1.0, 1.0)).to(t)
+    gain, dy = normal(g, D, dtype=dtype), normal(g, rows, D, dtype=dtype)
+    label = f"norm at {scale} D{D} {dtype}"
+    op = AddNorm(rows, D, dtype, eps)
+    y = torch.empty_like(s).cuda()
+    op.forward(s.cuda(), None, gain.cuda(), None, y)
+    ref = norm_definition(s, gain, eps)
+    close(y, ref, ref.abs(), STEPS, dtype, label + " y")
+    y8, scales = torch.zeros(rows, D, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(rows, device="cuda")
+    op.forward_q8(s.cuda(), None, gain.cuda(), None, y8, scales)
+    check_q8(y8, scales, ref, label + " 8 bits")
+    dx, dg = torch.full_like(s, float("nan")).cuda(), torch.full((D,), float("nan"), device="cuda")
+    op.backward(dy.cuda(), None, s.cuda(), gain.cuda(), dx, dg)
+    rdx, dsize, rdg, gsize = norm_gradient(s, gain, dy, None, eps)
+    close(dx, rdx, dsize, 3 * STEPS, dtype, label + " dx")
+    close(dg, rdg, gsize, STEPS + rows + 8, "f32", label + " dg")

@@ -337,8 +337,9 @@ hipError_t launch_norm_bwd(const NormBwdArgs &a, hipStream_t s)
     if (nv <= 256) return CALL(4, 1);          \
     if (nv <= 512) return CALL(4, 2);          \
     if (nv <= 1024) return CALL(4, 4);         \
-    if (nv <= 2048) return CALL(8, 4);         \
-    return CALL(16, 4);
+    if constexpr (NORM_MAX_D / VEC<T> > 2048)  \
+        if (nv > 2048) return CALL(16, 4);     \
+    return CALL(8, 4);
 
 template <typename T>
 hipError_t add_norm_t(const NormArgs &a, hipStream_t s)

@@ -448,12 +448,15 @@ __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(R
     for (int ti = 0; ti < TT; ++ti) rowf[ti] = r.inter * decay_pow(lg, 16 * ti + c16 + pre);
     float wc[E];          // the tokens' factors in the chunk's final state
     int wc_rows = -1;     // for a chunk of so many tokens
-    float whole = 1.0f;   // the state's factor over that chunk
     // The state is gain * X: a chunk's decay goes into gain, its tokens are
     // added divided by gain, and X is multiplied only when gain gets small
     // (one chunk in many for the usual decays; so X is at most 2^10 times the
-    // state)
+    // state).  gain is the power of the decay over all tokens since then: a
+    // product of the chunks' powers would have each one's rounding, the same one
+    // every time, which adds up to 1e-4 of the state of a head that remembers
+    // 65536 tokens.
     float gain = 1.0f;
+    int since = 0;
 
     Reader<CHA, T> ra;
     Reader<CHC, T> rc;
@@ -568,20 +571,21 @@ __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(R
         if (!OUT || t0 + C < end || XT) {
             if (rows != wc_rows) {
                 wc_rows = rows;
-                whole = decay_pow(lg, rows);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const int left = rows - 1 - (16 * (e / 4) + 4 * q + e % 4);
                     wc[e] = left < 0 ? 0.0f : r.update * decay_pow(lg, left + 1 - pre);
                 }
             }
-            gain *= whole;
+            since += rows;
+            gain = decay_pow(lg, since);
             if (__builtin_amdgcn_readfirstlane(gain < 0x1p-10f)) {
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) X[kt][mt] *= gain;
                 gain = 1.0f;
+                since = 0;
             }
             const float inv = 1.0f / gain;
             float w[E];
@@ -630,7 +634,8 @@ __global__ __launch_bounds__(512, DA <= 64 ? 3 : 2) void linattn_chunks_kernel(R
 }
 
 // Turns the slots into the states at the parts' starts.  A batch of them is read
-// before the first is written.
+// before the first is written.  The parts' decay multiplies in 64 bits, lest its
+// rounding add up over many parts (as a chunk's would, above).
 template <typename T>
 __global__ __launch_bounds__(256) void linattn_join_kernel(Roles<T> g)
 {
@@ -644,7 +649,7 @@ __global__ __launch_bounds__(256) void linattn_join_kernel(Roles<T> g)
     const int live = (n + g.part_len - 1) / g.part_len;   // slots 1 .. live - 1 are filled
     f32x4 *p = reinterpret_cast<f32x4 *>(r.slots + bh * g.parts * (long)size + e);
     f32x4 x = r.X0 ? *p : f32x4{0.f, 0.f, 0.f, 0.f};
-    const float keep = decay_pow(decay_log2(g.decay[bh % g.N]), g.part_len);
+    const double keep = exp2(log2((double)g.decay[bh % g.N]) * g.part_len);
     for (int k0 = 1; k0 < live; k0 += BATCH) {
         f32x4 add[BATCH];
 #pragma unroll
@@ -652,7 +657,11 @@ __global__ __launch_bounds__(256) void linattn_join_kernel(Roles<T> g)
             if (k0 + k < live) add[k] = p[(long)(k0 + k) * (size / 4)];
 #pragma unroll
         for (int k = 0; k < BATCH; ++k)
-            if (k0 + k < live) p[(long)(k0 + k) * (size / 4)] = x = keep * x + add[k];
+            if (k0 + k < live) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v) x[v] = (float)(keep * x[v] + add[k][v]);
+                p[(long)(k0 + k) * (size / 4)] = x;
+            }
     }
 }
 

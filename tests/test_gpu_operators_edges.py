@@ -259,3 +259,33 @@ def test_add_norm_at_the_ends_of_its_range(dtype, D, scale, eps):
     rdx, dsize, rdg, gsize = norm_gradient(s, gain, dy, None, eps)
     close(dx, rdx, dsize, 3 * STEPS, dtype, label + " dx")
     close(dg, rdg, gsize, STEPS + rows + 8, "f32", label + " dg")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [1, 3, 512])
+def test_linattn_long_memories(N, dtype):
+    """Heads that remember 32768 to 65536 tokens: the state of a sequence of
+    several times that, forwards and backwards; split into 2048 parts of a few
+    chunks, and (many heads) into 4 of thousands."""
+    T, K, M, some = 1 << 18, 8, 8, 64
+    g = torch.Generator(device="cuda").manual_seed(N)
+    lam = (1 - 2.0 ** -16 * (1 + (torch.arange(N) * 37 % 64) / 64)).float()
+    t = normal(gen(0), 1, dtype=dtype).dtype
+    k, v = ((0.5 + torch.rand(T, 1, N * w, generator=g, device="cuda")).to(t) for w in (K, M))
+    L = lam[:some].double().cuda()
+    age = torch.arange(T, dtype=torch.float64, device="cuda").flip(0)
+    weight = torch.exp(torch.log(L)[:, None] * age)                              # [N][T]
+    a, b = (x[:, 0, :some * w].double().view(T, -1, w).permute(1, 0, 2).contiguous() for x, w in ((k, K), (v, M)))
+    ref = torch.matmul((a * weight[..., None]).transpose(1, 2).contiguous(), b)  # [N][K][M]
+    # backwards the first token's state is decay^(t+1) of token t's product
+    back = torch.matmul((a * (weight.flip(1) * L[:, None])[..., None]).transpose(1, 2).contiguous(), b)
+    op = make_linattn(T, 1, N, K, M, dtype, False, 1.0)
+    o = torch.empty(T, 1, N * M, dtype=t, device="cuda")
+    ST, dS0 = (torch.empty(1, N, K, M, device="cuda") for _ in range(2))
+    op.forward(k, k, v, lam.cuda(), o, ST=ST)
+    op.backward(v, k, k, v, lam.cuda(), None, None, None, dS0=dS0)
+    # a state takes three roundings a chunk (16 or 32 tokens) that have no common sign: over the 65536
+    # tokens it remembers a walk of 3 * 4096 steps of up to u, 64 u in the mean square; six of them,
+    # and the powers' own errors, 20 u
+    for got, want, n in ((ST, ref, "ST"), (dS0, back, "dS0")):
+        close(got[0, :some], want.cpu(), want.cpu(), 6 * 64 + 20, "f32", f"long memory N{N} {dtype} {n}")

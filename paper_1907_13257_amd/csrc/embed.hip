@@ -146,7 +146,7 @@ __global__ __launch_bounds__(SORT_TILE) void rank_kernel(int N, long V, const in
 // first.  A pass is a count of each block's digits and a scatter; a block owns
 // `span` consecutive tokens.
 constexpr int SORT_MAX_BLOCKS = 256;
-constexpr int SORT_MAX_BITS = 11;      // of a digit: 2048 counters per wave of the block, 64 KiB of LDS
+constexpr int SORT_MAX_BITS = 11;      // of a digit: 2048 counters per wave of the block, with the digits' places 72 KiB of LDS
 
 struct SortPlan {
     int bits, passes, blocks;

@@ -5,11 +5,12 @@ sequences that are split, and the less travelled ways through a stack.
 Tolerances are those of test_gpu_operators: half a step of the storage type of
 the result, and d half steps of fp32 of the sum of its terms' sizes, d counted
 where it is used."""
-import numpy as np
 import pytest
 
 from _gpu_helpers import announce
-from test_gpu_operators import U, close, device_buffers, gen, linattn_case, make_linattn, normal, run_linattn
+import test_gpu_operators as basic
+from test_gpu_operators import (U, check_linattn, close, device_buffers, gen, linattn_case, make_linattn, normal,
+                                run_linattn)
 
 pytestmark = pytest.mark.gpu
 
@@ -289,3 +290,183 @@ def test_linattn_long_memories(N, dtype):
     # and the powers' own errors, 20 u
     for got, want, n in ((ST, ref, "ST"), (dS0, back, "dS0")):
         close(got[0, :some], want.cpu(), want.cpu(), 6 * 64 + 20, "f32", f"long memory N{N} {dtype} {n}")
+
+
+# ---------------------------------------------------------------------------
+# linear attention, sequences that are split: the only calls with a workspace
+# ---------------------------------------------------------------------------
+SPLIT_CASES = [   # T, dtype, parts of a sequence, forward and backward alike
+    (320, "bf16", 3),     # joined by their blocks
+    (160, "f32", 3),
+    (700, "bf16", 6),     # and by a launch of their own
+    (350, "f32", 6),
+]
+
+
+class SplitCase:
+    """Forward and backward of a split call on its own buffers; the workspace
+    says that it is split, and into how many parts."""
+
+    def __init__(self, T, dtype, parts, lengths="ragged", B=3, N=2, K=32, M=40, seed=0):
+        self.shape = T, B, N, K, M, dtype
+        self.c = linattn_case(T, B, N, K, M, dtype, lengths, True, seed=seed)
+        self.d = device_buffers(self.c, T, B, N, K, M, dtype, True, poison=False)
+        self.op = make_linattn(T, B, N, K, M, dtype, True)
+        assert self.op.ws_bytes == 2 * parts * B * N * K * M * 4
+
+    def run(self):
+        return run_linattn(self.op, self.d)
+
+    def check(self, got, label):
+        T, B, N, K, M, dtype = self.shape
+        check_linattn(got, self.c, T, B, N, K, M, dtype, K ** -0.5, label)
+
+    def outs(self):
+        return {n: self.d[n] for n in ("o", "ST", "dq", "dk", "dv", "dS0")}
+
+    def clear(self):
+        for t in list(self.outs().values()) + [self.op.workspace]:
+            t.fill_(1)
+
+
+def same(got, want, label=""):
+    for n in want:
+        assert torch.equal(got[n], want[n]), (label, n)
+
+
+def copies(tensors):
+    return {n: t.clone() for n, t in tensors.items()}
+
+
+@pytest.mark.parametrize("T,dtype,parts", SPLIT_CASES)
+def test_linattn_split_states_in_place(T, dtype, parts):
+    """Final states over initial ones, and each gradient alone, in the bits of
+    the call with everything apart: the first states are read from the
+    workspace, since another block may have replaced them."""
+    s = SplitCase(T, dtype, parts)
+    d = s.d
+    want = copies(s.run())
+    s.check(want, f"split T{T} {dtype}")
+    for n in ("dq", "dk", "dv", "dS0"):
+        s.clear()
+        only = [d[m] if m == n else None for m in ("dq", "dk", "dv", "dS0")]
+        s.op.backward(d["do"], d["q"], d["k"], d["v"], d["decay"], *only[:3], d["lengths"], d["S0"], d["dST"], only[3])
+        assert torch.equal(d[n], want[n]), n
+    S, G = d["S0"].clone(), d["dST"].clone()
+    s.clear()
+    s.op.forward(d["q"], d["k"], d["v"], d["decay"], d["o"], d["lengths"], S, S)
+    assert torch.equal(S, want["ST"]) and torch.equal(d["o"], want["o"])
+    s.op.backward(d["do"], d["q"], d["k"], d["v"], d["decay"], d["dq"], d["dk"], d["dv"], d["lengths"], d["S0"], G, G)
+    same(dict(dq=d["dq"], dk=d["dk"], dv=d["dv"], dS0=G), {n: want[n] for n in ("dq", "dk", "dv", "dS0")})
+
+
+@pytest.mark.parametrize("T,dtype,parts", SPLIT_CASES)
+def test_linattn_split_lengths_at_the_parts_ends(T, dtype, parts):
+    """Sequences that end where a part does, one token before and after, in the
+    first part, and not at all; rows behind the end hold NaN and get zeros."""
+    chunk = 32 if dtype == "bf16" else 16
+    part = ((T + chunk - 1) // chunk + parts - 1) // parts * chunk
+    lengths = torch.tensor([0, 1, part - 1, part, part + 1, 2 * part, 2 * part + 1, T - 1, T], dtype=torch.int32)
+    B, N, K, M = len(lengths), 1, 16, 24
+    c = linattn_case(T, B, N, K, M, dtype, "ragged", True)
+    c["lengths"] = lengths
+    op = make_linattn(T, B, N, K, M, dtype, False)
+    assert op.ws_bytes == 2 * parts * B * N * K * M * 4
+    op.workspace.fill_(255)   # NaN: nothing is read that was not written
+    d = device_buffers(c, T, B, N, K, M, dtype, False)
+    check_linattn(run_linattn(op, d), c, T, B, N, K, M, dtype, K ** -0.5, f"ends of parts T{T} {dtype}")
+    assert torch.equal(d["ST"][0].cpu(), c["S0"][0]) and torch.equal(d["dS0"][0].cpu(), c["dST"][0])
+    for n in ("o", "dq", "dk", "dv"):
+        for b in range(B):
+            assert not d[n][int(lengths[b]):, b].any(), (n, b)
+
+
+@pytest.mark.parametrize("T,dtype,parts", SPLIT_CASES)
+def test_linattn_split_on_another_stream(T, dtype, parts):
+    s = SplitCase(T, dtype, parts)
+    want = copies(s.run())
+    s.clear()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        s.run()
+    torch.cuda.current_stream().wait_stream(side)
+    same(s.outs(), want)
+
+
+@pytest.mark.parametrize("T,dtype,parts", SPLIT_CASES)
+def test_linattn_split_captured_and_replayed(T, dtype, parts):
+    """Captured once, replayed with other inputs and lengths between eager runs."""
+    s = SplitCase(T, dtype, parts)
+    s.run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.run()
+    for k in range(4):
+        s.d["q"].mul_(-0.5)
+        s.d["S0"].add_(1)
+        s.d["lengths"].copy_(s.d["lengths"].roll(1))
+        s.clear()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = copies(s.outs())
+        s.clear()
+        same(got, s.run(), k)
+
+
+@pytest.mark.parametrize("T,dtype,parts", SPLIT_CASES)
+def test_linattn_split_graphs_and_eager_calls_at_once(T, dtype, parts):
+    """Two objects' graphs on two streams beside a third's eager calls: each has
+    its own workspace, and gives what it gives alone."""
+    cases = [SplitCase(T, dtype, parts, seed=k) for k in range(3)]
+    want, graphs = [], []
+    for s in cases:
+        want.append(copies(s.run()))
+    torch.cuda.synchronize()
+    for s in cases[:2]:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            s.run()
+        graphs.append(graph)
+        s.clear()
+    streams = [torch.cuda.Stream() for _ in graphs]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for st, graph in zip(streams, graphs):
+            with torch.cuda.stream(st):
+                graph.replay()
+        cases[2].run()
+    torch.cuda.synchronize()
+    for k, s in enumerate(cases):
+        same(s.outs(), want[k], k)
+
+
+@pytest.mark.parametrize("T,dtype,parts", SPLIT_CASES)
+def test_linattn_split_prompt_then_steps(T, dtype, parts):
+    """A split prompt whose final states replace the first ones, then single
+    tokens: the outputs of the whole sequence."""
+    B, N, K, M, more = 3, 2, 32, 40, 5
+    c = linattn_case(T + more, B, N, K, M, dtype, None, True)
+    d = device_buffers(c, T + more, B, N, K, M, dtype, False)
+    prompt, step = make_linattn(T, B, N, K, M, dtype, False), make_linattn(1, B, N, K, M, dtype, False)
+    assert prompt.ws_bytes == 2 * parts * B * N * K * M * 4
+    S = d["S0"]
+    prompt.forward(d["q"][:T], d["k"][:T], d["v"][:T], d["decay"], d["o"][:T], S0=S, ST=S)
+    for t in range(T, T + more):
+        step.step(d["q"][t], d["k"][t], d["v"][t], d["decay"], S, S, d["o"][t])
+    check_linattn(dict(o=d["o"], ST=S), c, T + more, B, N, K, M, dtype, K ** -0.5, f"split prompt and steps T{T} {dtype}")
+
+
+# ---------------------------------------------------------------------------
+# embedding: the widest digits of the sort
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("N,V,D,dtype", [
+    (9001, 2047, 8, "bf16"),           # one digit of eleven bits: every thread has two counters
+    (9001, 2048, 8, "f32"),            # the first rows that need a second digit
+    (9001, 1 << 21, 8, "bf16"),        # two digits of eleven bits
+    (70001, (1 << 22) - 1, 8, "f32"),  # the last rows that two digits reach
+    (9001, 1 << 22, 8, "bf16"),        # and the first that need three
+])
+def test_embedding_sorted_by_wide_digits(N, V, D, dtype):
+    basic.test_embedding(N, V, D, dtype, 0, "mixed")

@@ -470,3 +470,112 @@ def test_linattn_split_prompt_then_steps(T, dtype, parts):
 ])
 def test_embedding_sorted_by_wide_digits(N, V, D, dtype):
     basic.test_embedding(N, V, D, dtype, 0, "mixed")
+
+
+# ---------------------------------------------------------------------------
+# stacks: an embedding below the layer wavefront; norms on other kinds of layers
+# ---------------------------------------------------------------------------
+def test_embedding_below_a_wavefront_stack():
+    """The layer wavefront takes an embedding's rows as it takes any input: the
+    same bits as the stack without an embedding on those rows, and the table's
+    gradient of its input gradient, over two mini-batches."""
+    from paper_1907_13257_amd import Embedding, Stack, StackLayer
+    T, B, H, V, scale = 6, 16, 1024, 50, 2.0
+    g = gen(51)
+    layers = [StackLayer(H, H), StackLayer(H, H, residual=True), StackLayer(H, H, residual=True)]
+    params = [[dict(W=normal(g, 4 * H, H, scale=0.05).cuda(), R=normal(g, 4 * H, H, scale=0.05).cuda(),
+                    b=normal(g, 4 * H, dtype="f32", scale=0.05).cuda())] for _ in layers]
+    table, dout = normal(g, V, H, scale=0.5).cuda(), normal(g, T, B, H).cuda()
+    whole, plain = Stack(T, B, layers, vocab=V, embed_scale=scale), Stack(T, B, layers)
+    E = Embedding(T * B, V, H, scale=scale)
+    rows = torch.empty(T, B, H, dtype=torch.bfloat16, device="cuda")
+    grads, want = whole.alloc_grads(params), plain.alloc_grads(params)
+    dtable, wtable = (torch.full((V, H), float("nan"), device="cuda") for _ in range(2))
+    for k in range(2):
+        ids = torch.randint(-1, V, (T, B), generator=g).cuda()
+        out = whole.forward(ids, params, table=table)
+        dx = whole.backward(dout, params, grads, accumulate=k > 0, dtable=dtable)
+        assert whole.last_forward == whole.last_backward == "wavefront"
+        E.forward(ids, table, rows)
+        assert torch.equal(plain.forward(rows, params), out)
+        assert plain.last_forward == "wavefront"
+        assert torch.equal(plain.backward(dout, params, want, accumulate=k > 0), dx)
+        E.backward(ids, dx, wtable, accumulate=k > 0)
+        assert whole.check() == plain.check() == 0
+    assert torch.equal(dtable, wtable) and dtable.any()
+    for a, b in zip(grads, want):
+        for n in a[0]:
+            assert torch.equal(a[0][n], b[0][n]), n
+
+
+def lstm_definition(x, p, reverse):
+    """One direction of an LSTM or LSTMP layer in 64 bits, gates in the order i, f, g, o."""
+    T, B, _ = x.shape
+    H = p["R"].shape[0] // 4
+    c = torch.zeros(B, H, dtype=torch.float64)
+    h = torch.zeros(B, p["R"].shape[1], dtype=torch.float64)
+    ys = [None] * T
+    for t in reversed(range(T)) if reverse else range(T):
+        i, f, z, o = (x[t] @ p["W"].t() + h @ p["R"].t() + p["b"]).split(H, 1)
+        c = torch.sigmoid(f) * c + torch.sigmoid(i) * torch.tanh(z)
+        h = torch.sigmoid(o) * torch.tanh(c)
+        if "P" in p:
+            h = h @ p["P"].t()
+        ys[t] = h
+    return torch.stack(ys)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norms_on_bidirectional_and_projected_layers(dtype):
+    """Norms on a bidirectional layer, a projected one and one that is both,
+    with a residual layer without a norm among them; against the same network
+    in 64 bits differentiated by torch, with the LSTM stack's tolerances."""
+    from _gpu_helpers import TOL, normwise
+    from paper_1907_13257_amd import Stack, StackLayer
+    T, B, W, V, eps = 9, 5, 64, 31, 1e-3
+    kinds = [dict(H=32, bidirectional=True, residual=True, norm=True), dict(H=96, Hp=64, residual=True, norm=True),
+             dict(H=64, residual=True), dict(H=48, Hp=32, bidirectional=True, residual=True, norm=True), dict(H=64)]
+    g = gen(61)
+    layers = [StackLayer(W, **kw) for kw in kinds]
+    params = []
+    for L in layers:
+        dirs = []
+        for d in range(2 if L.bidirectional else 1):
+            p = dict(W=normal(g, 4 * L.H, W, dtype=dtype, scale=0.1), R=normal(g, 4 * L.H, L.Hr, dtype=dtype, scale=0.1),
+                     b=normal(g, 4 * L.H, dtype="f32", scale=0.1))
+            if L.Hp:
+                p["P"] = normal(g, L.Hp, L.H, dtype=dtype, scale=0.2)
+            if L.norm and d == 0:
+                p["g"] = normal(g, W, dtype=dtype, scale=0.3) + 1
+            dirs.append(p)
+        params.append(dirs)
+    table, dout = normal(g, V, W, dtype=dtype, scale=0.5), normal(g, T, B, W, dtype=dtype)
+    ids = torch.randint(-1, V, (T, B), generator=g)
+
+    leaves = [[{n: t.double().requires_grad_(True) for n, t in p.items()} for p in dirs] for dirs in params]
+    tab = table.double().requires_grad_(True)
+    cur = carry = torch.where((ids >= 0)[:, :, None], tab[ids.clamp(min=0)], 0.0)
+    for L, dirs in zip(layers, leaves):
+        y = torch.cat([lstm_definition(cur, p, d == 1) for d, p in enumerate(dirs)], 2)
+        y = y + carry if L.residual else y
+        cur = carry = y
+        if L.norm:
+            cur = y / torch.sqrt((y * y).mean(2, keepdim=True) + eps) * dirs[0]["g"]
+    cur.backward(dout.double())
+
+    stack = Stack(T, B, layers, dtype, vocab=V, eps=eps)
+    dev = [[{n: t.cuda() for n, t in p.items()} for p in dirs] for dirs in params]
+    grads, dtable = stack.alloc_grads(dev), torch.full((V, W), float("nan"), device="cuda")
+    out = stack.forward(ids.cuda(), dev, table=table.cuda())
+    stack.backward(dout.cuda(), dev, grads, dtable=dtable)
+    assert stack.check() == 0 and stack.last_forward == "layers"
+    errs = {"out": (normwise(out.double().cpu(), cur.detach()), "out"),
+            "table": (normwise(dtable.double().cpu(), tab.grad), "grad")}
+    for li, dirs in enumerate(grads):
+        for d, gd in enumerate(dirs):
+            for n, t in gd.items():
+                errs[f"{n}{li}.{d}"] = (normwise(t.double().cpu(), leaves[li][d][n[1:]].grad), "grad")
+    assert {n for n in errs if n.startswith("dg")} == {"dg0.0", "dg1.0", "dg3.0"}
+    announce(f"norms on other layers {dtype}: " + ", ".join(f"{k}={v:.1e}" for k, (v, _) in errs.items()))
+    bad = {k: v for k, (v, kind) in errs.items() if not v <= TOL[dtype][kind]}
+    assert not bad, bad

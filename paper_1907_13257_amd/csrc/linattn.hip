@@ -674,11 +674,19 @@ struct SplitPlan {
 // none shorter than MIN_CHUNKS chunks.  A wave has 32 columns: P and the shared
 // rows cost a wave the same for 16.  Where that leaves the SIMDs with less than
 // one wave each unsplit and few chunks in all (FEW_CHUNKS of a wave per SIMD),
-// time is the latency of a wave's chunks, and 16 columns halve it: 2 x 1999
-// tokens of 16 heads of 64 in 36 us with 32 columns and 30 with 16, 12 x 333 of
-// 5 heads in fp32, forward and backward, 91 and 83; but 128 x 50 tokens of 16
-// heads 51 and 59, 4 x 4096 of 16 heads of 128 396 and 511.  Heads wider than
-// 128 always take 16: twice the state does not fit the registers.
+// time is the latency of a wave's chunks, and 16 columns shorten it, up to heads
+// of 64 (bf16) or 80 (fp32); wider ones would make more waves than a block's
+// SIMDs take at a time.  Forward or backward in us with 32 and with 16 columns:
+//   2 x 1999 tokens, 16 heads of 64                   forward 35, 31   backward 50, 54
+//   8, 24 x 200, 16 heads of 64                       forward 18, 15 and 26, 22
+//   32, 64 x 200 (too many waves)                     forward 29, 28 and 26, 30
+//   4, 8 x 1000, 16 heads of 64                       forward 34, 28 and 40, 40
+//   4, 16 x 1000 (the second has too many)            backward 51, 53 and 98, 105
+//   4 x 700, 8 heads of 72, 96                        forward 30, 29 and 32, 32   backward 47, 56 and 51, 65
+//   4 x 1000, 8 heads of 128                          forward 38, 37   backward 77, 96
+//   12 x 333, 5 heads of 40 and 72, fp32              forward 30, 31   backward 76, 69
+//   4 x 333, 8 heads of 80, 88, 128, fp32             backward 57, 57 and 59, 63 and 73, 92
+// Heads wider than 128 always take 16: twice the state does not fit the registers.
 constexpr int MAX_WAVES = 8;   // of a block
 constexpr int TARGET_WAVES = 2048, MIN_CHUNKS = 3, FEW_CHUNKS = 16, SIMDS = 1024;
 SplitPlan split_plan(const LinAttnShape &sh, int chunk, int roles)
@@ -692,7 +700,8 @@ SplitPlan split_plan(const LinAttnShape &sh, int chunk, int roles)
     if (parts < 1) parts = 1;
     const int per = (int)((chunks + parts - 1) / parts);
     const bool few = waves < SIMDS && waves * chunks < (long)FEW_CHUNKS * SIMDS;
-    return SplitPlan{(chunks + per - 1) / per, per * chunk, few || width > 128 ? 1 : 2};
+    const bool narrow = width <= (chunk == Mat<bf16_t>::C ? 64 : 80);
+    return SplitPlan{(chunks + per - 1) / per, per * chunk, (few && narrow) || width > 128 ? 1 : 2};
 }
 
 // The blocks of a head (its roles; the columns of a wide one), which read the

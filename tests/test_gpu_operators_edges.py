@@ -579,3 +579,18 @@ def test_norms_on_bidirectional_and_projected_layers(dtype):
     announce(f"norms on other layers {dtype}: " + ", ".join(f"{k}={v:.1e}" for k, (v, _) in errs.items()))
     bad = {k: v for k, (v, kind) in errs.items() if not v <= TOL[dtype][kind]}
     assert not bad, bad
+
+
+@pytest.mark.parametrize("T,B,N,K,M,dtype,lengths,states,fused", [
+    (100, 2, 2, 128, 144, "bf16", "ragged", True, True),   # keys of 97 .. 128 with values wider than 128
+    (70, 1, 2, 88, 136, "bf16", None, True, False),
+    (70, 1, 2, 120, 136, "f32", "ragged", True, False),
+    (90, 2, 1, 96, 200, "f32", None, False, True),
+    (200, 2, 2, 72, 64, "bf16", "ragged", True, False),    # few heads on both sides of 64 and of 80
+    (200, 2, 2, 64, 64, "bf16", "ragged", True, False),
+    (100, 2, 2, 80, 64, "f32", "ragged", True, False),
+    (100, 2, 2, 64, 88, "f32", "ragged", True, False),
+    (100, 2, 2, 128, 128, "f32", "ragged", True, True),
+])
+def test_linattn_widths_around_the_waves_columns(T, B, N, K, M, dtype, lengths, states, fused):
+    basic.test_linattn(T, B, N, K, M, dtype, lengths, states, fused)

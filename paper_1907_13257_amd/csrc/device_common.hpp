@@ -92,6 +92,27 @@ __device__ __forceinline__ void mfma32(f32x16 &acc, u32x4 a, u32x4 b, float)
 __device__ __forceinline__ u32x4 ldg16(const void *p) { return *reinterpret_cast<const u32x4 *>(p); }
 __device__ __forceinline__ u32x4 zero16() { return u32x4{0u, 0u, 0u, 0u}; }
 
+// The elements of a 16-byte access, and their fp32 values.
+template <typename T> constexpr int VEC = 16 / (int)sizeof(T);
+template <typename T>
+__device__ __forceinline__ void unpack(u32x4 v, float (&f)[VEC<T>])
+{
+    T e[VEC<T>];
+    __builtin_memcpy(e, &v, 16);
+#pragma unroll
+    for (int i = 0; i < VEC<T>; ++i) f[i] = to_f32(e[i]);
+}
+template <typename T>
+__device__ __forceinline__ u32x4 pack(const float (&f)[VEC<T>])
+{
+    T e[VEC<T>];
+#pragma unroll
+    for (int i = 0; i < VEC<T>; ++i) e[i] = from_f32<T>(f[i]);
+    u32x4 v;
+    __builtin_memcpy(&v, e, 16);
+    return v;
+}
+
 // ---------------------------------------------------------------------------
 // Direct global -> LDS loads.  A buffer descriptor covers [base, base+bytes);
 // loads past its end return zero.  buffer_load_dwordx4 ... lds writes lane

@@ -7,28 +7,6 @@ namespace lstm355 {
 
 namespace {
 
-template <typename T> constexpr int VEC = 16 / (int)sizeof(T);   // elements of a 16-byte access
-
-template <typename T>
-__device__ __forceinline__ void unpack(u32x4 v, float (&f)[VEC<T>])
-{
-    T e[VEC<T>];
-    __builtin_memcpy(e, &v, 16);
-#pragma unroll
-    for (int i = 0; i < VEC<T>; ++i) f[i] = to_f32(e[i]);
-}
-
-template <typename T>
-__device__ __forceinline__ u32x4 pack(const float (&f)[VEC<T>])
-{
-    T e[VEC<T>];
-#pragma unroll
-    for (int i = 0; i < VEC<T>; ++i) e[i] = from_f32<T>(f[i]);
-    u32x4 v;
-    __builtin_memcpy(&v, e, 16);
-    return v;
-}
-
 // Lanes that share a row: the power of two that covers its vectors, 64 at most.
 int lanes_per_row(int nv)
 {

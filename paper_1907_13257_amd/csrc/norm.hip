@@ -7,28 +7,10 @@ namespace lstm355 {
 
 namespace {
 
-template <typename T> constexpr int VEC = 16 / (int)sizeof(T);   // elements of a 16-byte access
-
 template <typename T>
-__device__ __forceinline__ void load_vec(const T *p, float (&f)[VEC<T>])
-{
-    T e[VEC<T>];
-    const u32x4 v = ldg16(p);
-    __builtin_memcpy(e, &v, 16);
-#pragma unroll
-    for (int i = 0; i < VEC<T>; ++i) f[i] = to_f32(e[i]);
-}
-
+__device__ __forceinline__ void load_vec(const T *p, float (&f)[VEC<T>]) { unpack<T>(ldg16(p), f); }
 template <typename T>
-__device__ __forceinline__ void store_vec(T *p, const float (&f)[VEC<T>])
-{
-    T e[VEC<T>];
-#pragma unroll
-    for (int i = 0; i < VEC<T>; ++i) e[i] = from_f32<T>(f[i]);
-    u32x4 v;
-    __builtin_memcpy(&v, e, 16);
-    *reinterpret_cast<u32x4 *>(p) = v;
-}
+__device__ __forceinline__ void store_vec(T *p, const float (&f)[VEC<T>]) { *reinterpret_cast<u32x4 *>(p) = pack<T>(f); }
 
 // 8 (bf16 storage) or 4 (fp32) values as e4m3 bytes, round to nearest even.
 __device__ __forceinline__ unsigned e4m3x4(float a, float b, float c, float d)

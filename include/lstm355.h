@@ -290,8 +290,9 @@ size_t lstm_embed_workspace_size(long N, long V, int D);
  *   accumulate: 0 overwrites the whole table's gradient (rows that no token
  *     picks with zeros), 1 adds to it and touches only rows that are picked.
  * Tokens outside 0 .. V-1 take no part.  Each row is summed in fp32 over its
- * tokens sorted by position, in an order set by the sizes alone: equal inputs
- * give equal bits.  N = 0 is allowed.  N and V up to 2^31 - 2^20. */
+ * tokens sorted by position.  Equal inputs give equal bits; how a row's sum is
+ * grouped depends on the row's place among all sorted tokens, so other tokens
+ * may change its last bits.  N = 0 is allowed.  N and V up to 2^31 - 2^20. */
 lstm_status_t lstm_embed_backward(lstm_dtype_t dtype, long N, long V, int D, const int64_t *ids, const void *dout,
                                   long ldo, float scale, float *dtable, int accumulate, void *workspace,
                                   size_t workspace_bytes, void *stream);
@@ -338,7 +339,8 @@ lstm_status_t lstm_add_norm_backward(lstm_dtype_t dtype, long rows, int D, const
  *   q, k [T][B][N*K], v, o [T][B][N*M] (head n in columns n*K.. or n*M..), row
  *   strides ldq, ldk, ldv, ldo between consecutive (t,b) rows: columns of one
  *   fused projection may be given.  decay [N] fp32, every value in 0 .. 1
- *   (constants of the layer: they get no gradient).  States [B][N][K][M] fp32.
+ *   (constants of the layer: they get no gradient).  States [B][N][K][M] fp32,
+ *   up to 1e35 in size (a sequence holds them up to 2^10 times as large).
  * A value that is not finite spreads within its sequence and head only, but
  * there also to outputs up to 31 steps before it (a chunk's sum multiplies what
  * it leaves out by zero). */

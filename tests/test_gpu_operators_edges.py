@@ -594,3 +594,24 @@ def test_norms_on_bidirectional_and_projected_layers(dtype):
 ])
 def test_linattn_widths_around_the_waves_columns(T, B, N, K, M, dtype, lengths, states, fused):
     basic.test_linattn(T, B, N, K, M, dtype, lengths, states, fused)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_linattn_wide_heads_captured(dtype):
+    """The widest heads, whose blocks ask for more shared memory than a launch
+    has by default: captured as their first call on these sizes, then replayed."""
+    T, B, N, K, M = 75, 2, 1, 256, 248
+    c = linattn_case(T, B, N, K, M, dtype, "ragged", True)
+    d = device_buffers(c, T, B, N, K, M, dtype, False)
+    op = make_linattn(T, B, N, K, M, dtype, False)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run_linattn(op, d)
+    for _ in range(3):
+        for n in ("o", "ST", "dq", "dk", "dv", "dS0"):
+            d[n].fill_(1)
+        graph.replay()
+        torch.cuda.synchronize()
+        check_linattn({n: d[n] for n in ("o", "ST", "dq", "dk", "dv", "dS0")}, c, T, B, N, K, M, dtype, K ** -0.5,
+                      f"captured wide heads {dtype}")

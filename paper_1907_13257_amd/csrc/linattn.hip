@@ -74,13 +74,12 @@ __device__ __forceinline__ int sequence_length(const int32_t *lengths, int b, in
 // reads) come from LDS.  Every wave forms P for itself.
 //
 // bf16 storage: X, P and the decayed C are fp32 values that the matrix cores
-// take in three bf16 parts, bf16(x), bf16(x - first) and bf16 of what is left:
-// eight bits each, so nothing of an fp32 value is left out and results are those
-// of fp32 factors, whichever states a call gives or wants.  (Two parts, which
-// leave out 2^-17 of a factor, take 395 us instead of 474 for 4 x 4096 tokens of
-// 16 heads of 128, forward and backward, 51 instead of 57 for 128 x 50 of 16 heads
-// of 64, 31 and 31 for 2 x 1999; but where terms cancel, the result's own rounding
-// is below what they lose.)
+// take in three bf16 parts of eight bits each, so nothing of a value is left out
+// and results are those of fp32 factors, whichever states a call gives or wants.
+// (Two parts, which leave out 2^-17 of a factor, take 395 us instead of 460 for 4 x
+// 4096 tokens of 16 heads of 128, forward and backward, 51 instead of 57 for 128 x
+// 50 of 16 heads of 64, 31 and 31 for 2 x 1999; but where terms cancel, the
+// result's own rounding is below what they lose.)
 //
 // What bounds it: with the chip full (two waves per SIMD at heads of 128), a
 // forward of 4 x 4096 tokens of 16 heads of 128 takes 70 us for 268 MB, 3.8 TB/s
@@ -270,23 +269,24 @@ __device__ __forceinline__ unsigned pack_bf16(float a, float b)   // one convers
     return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2{a, b}), bf16x2));
 }
 
-// fp32 values of an operand as the parts the matrix cores take.
+// fp32 values of an operand as the parts the matrix cores take.  A part is the
+// upper half of what the parts before it left over: eight bits of the value, cut
+// off and not rounded, so the three of them are the value and the largest values
+// stay finite.
 template <int NP>
 __device__ __forceinline__ void split(const float (&x)[8], u32x4 (&f)[NP], bf16_t)
 {
-    float r[NP][8];
+    unsigned r[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[0][e] = x[e];
+    for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(x[e]);
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) f[p][e / 2] = pack_bf16(r[p][e], r[p][e + 1]);
+        for (int e = 0; e < 8; e += 2) f[p][e / 2] = __builtin_amdgcn_perm(r[e + 1], r[e], 0x07060302u);
         if (p + 1 < NP)   // what is left over, exactly
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                r[p + 1][e] = r[p][e] - __uint_as_float(f[p][e / 2] << 16);
-                r[p + 1][e + 1] = r[p][e + 1] - __uint_as_float(f[p][e / 2] & 0xffff0000u);
-            }
+            for (int e = 0; e < 8; ++e)
+                r[e] = __float_as_uint(__uint_as_float(r[e]) - __uint_as_float(r[e] & 0xffff0000u));
     }
 }
 template <int NP>

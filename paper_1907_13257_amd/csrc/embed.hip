@@ -16,8 +16,9 @@ int lanes_per_row(int nv)
 }
 
 // out[n] = scale * table[ids[n]]; `lpr` lanes per row, one row after another, 16
-// bytes a lane.  Bound by memory: 40000 rows of 1024 bf16 in 28 us (164 MB, 5.9
-// TB/s), 6400 in 4.4; 16 rows in 2.0 us, a launch's latency.
+// bytes a lane.  Bound by memory: 40000 rows of 1024 bf16 in 28 to 32 us (164 MB, of
+// which 127 reach memory, at 4.0 TB/s), 6400 in 4.4 to 5.7; 16 rows in 2.1 us, a
+// launch's latency.
 template <typename T>
 __global__ __launch_bounds__(256) void embed_forward_kernel(long N, long V, int nv, const int64_t *__restrict__ ids,
                                                             const T *__restrict__ table, float scale,
@@ -45,7 +46,7 @@ __global__ __launch_bounds__(256) void embed_forward_kernel(long N, long V, int 
 // sort takes a share of the work beside it that needs no order: the zeros of an
 // overwritten gradient, written by blocks behind the sorting ones, so that the
 // sort's few blocks and their latency hide behind those stores (6400 tokens and
-// 32000 rows of 1024: 21 us, the 131 MB of zeros at 6.2 TB/s; zeros and a radix
+// 32000 rows of 1024: 22 us, the 131 MB of zeros at 6.0 TB/s; zeros and a radix
 // sort one after the other took 18 and 17 us).
 // ---------------------------------------------------------------------------
 constexpr int SORT_TILE = 1024;        // threads of a sorting block, tokens sorted at a time

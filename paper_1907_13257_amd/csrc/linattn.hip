@@ -81,16 +81,18 @@ __device__ __forceinline__ int sequence_length(const int32_t *lengths, int b, in
 // 50 of 16 heads of 64, 31 and 31 for 2 x 1999; but where terms cancel, the
 // result's own rounding is below what they lose.)
 //
-// What bounds it: with the chip full (two waves per SIMD at heads of 128), a
-// forward of 4 x 4096 tokens of 16 heads of 128 takes 70 us for 268 MB, 3.8 TB/s
-// against 4.85 of a copy; what is left is the chain of a wave's instructions:
-// per chunk and wave 84 matrix instructions and some 400 others, the split of X
-// the most of them (41 % of a wave's time it issues, 31 % it waits its turn to,
-// 28 % for data and barriers), and the registers of a 128-wide state allow no
-// third wave to fill the gaps.  The three gradients read 9 and write 3 widths of
-// rows where 4 and 3 would do: 250 us for 805 MB; one launch that formed all
-// three would have to run the tokens in both directions.  Short or few sequences
-// are bound by latency: about 2 us per chunk and 5 before the first.
+// What bounds it: with the chip full (two waves per SIMD at heads of 128), the
+// chain of a wave's instructions: per chunk and wave 120 matrix instructions and
+// some 700 others, the split of X and P the most of them (46 to 49 % of a wave's
+// time in the main launch it issues, 32 to 34 % it waits its turn to, 17 to 22 % for
+// data and barriers), and the registers of a 128-wide state allow no third wave to
+// fill the gaps.  A forward of 4 x 4096 tokens of 16 heads of 128 takes 121 us for
+// 268 MB, 2.2 TB/s against 4.9 of a copy, in three launches: the parts' states (35),
+// their join (11) and the outputs (83, each by itself under a profiler).  The three
+// gradients read 9 and write 3 widths of rows where 4 and 3 would do: 342 us for 805
+// MB, 61 of them for the parts' states; one launch that formed all three would have
+// to run the tokens in both directions.  Short or few sequences are bound by
+// latency: about 2 us per chunk and 5 before the first.
 // ---------------------------------------------------------------------------
 template <typename T> struct Mat;
 template <> struct Mat<bf16_t> {
@@ -706,12 +708,14 @@ SplitPlan split_plan(const LinAttnShape &sh, int chunk, int roles)
 
 // The blocks of a head (its roles; the columns of a wide one), which read the
 // same rows, are launched eight apart where they have many chunks: on one XCD at
-// about one time, so that its L2 serves what another of them has read.  Forward
-// and backward of 64 x 400 tokens of 16 heads of 64 in 190 us, else 200; 16 x 1000
-// of 8 heads of 128 183 and 201, of 4 heads of 256 409 and 428; 4 x 4096 of 16
-// heads of 128 394 and 397.  Short blocks stay one role after
-// another: 128 x 50 tokens of 16 heads of 64 in 55 us grouped and 53 not, 64 x 200
-// 96 and 96.
+// about one time, so that its L2 serves what another of them has read.  Backward in
+// us so and role after role, by a block's chunks: 8 (64 x 256 tokens of 16 heads of
+// 64) 69 and 72, 13 (64 x 400) 138 and 138, 16 (16 x 1000 of 8 heads of 128) 142 and
+// 161, 43 (4 x 4096 of 16 of 128) 341 and 349; of 4 heads of 256, 8 chunks, forward
+// 142 and 151, backward 315 and 325.  Short blocks stay one role after another: 2
+// chunks (128 x 50 of 16 heads of 64) 39 and 39, 4 (64 x 100) 36 and 35, 7 (64 x 200)
+// 63 and 63, 7 (32 x 200 of 8 of 128) 50 and 48; for heads of 256 the order pays from
+// 4 chunks on (16 x 300, forward 61 and 65).
 constexpr int GROUP_CHUNKS = 8;
 template <typename T, int DA, bool OUT, int MT>
 hipError_t launch_chunks(Roles<T> g, int roles, int width, hipStream_t s)
@@ -765,8 +769,14 @@ hipError_t launch_roles(const Roles<T> &g, int roles, hipStream_t s)
 
 // Parts from which on their states are joined by a launch of its own.  A block's
 // own joins cost it up to 1 us each, one after another; the launch takes 5 to
-// 11 us (21 parts of 2 x 1999 tokens: 30 us with the launch and 40 without; the
-// backward pass of 12 x 333 in 4 parts, with its forward, 87 and 83).
+// 11 us.  Us joined by the blocks and by the launch:
+//   heads of 64    forward   7 parts 22, 28 and 33, 33   10 29, 31   13 39, 36   21 36, 31
+//                  backward  3 parts 55, 57   5 42, 45   6 56, 58 and 65, 61   11 66, 54
+//   heads of 128   forward   4 parts 30, 35   7 39, 39   10 52, 45   16 74, 54
+//                  backward  4 parts 60, 54   5 76, 67   6 96, 84 and 132, 114
+//   40 x 72, fp32  forward   4 parts 22, 24   7 23, 22   8 28, 26   13 37, 35
+//                  backward  4 parts 33, 35   7 45, 44   8 64, 55
+// The larger a state and the more roles, the sooner the launch pays.
 constexpr int JOIN_PARTS = 6;
 template <typename T>
 hipError_t launch_join(const Roles<T> &g, int roles, hipStream_t s)

@@ -63,8 +63,8 @@ __device__ __forceinline__ float inverse_root(float squares, int D, float eps)  
 // A row is held in registers by W waves, P vectors per thread (thread t has
 // vectors t, t + 64 W, ...), so it is read once and both sums over it need no
 // second pass.  A block has four rows where a row is one wave's, else one.
-// Bound by memory: 6400 rows of 1024 bf16 in 8.8 us (52 MB, 5.9 TB/s), 20001 of
-// 8192 with the 8-bit output in 211 us (1.15 GB, 5.4 TB/s); 16 rows in 3.4 us.
+// Bound by memory: 6400 rows of 1024 bf16 in 10.2 us (52 MB, 5.1 TB/s), 20001 of
+// 8192 with the 8-bit output in 213 us (1.15 GB, 5.4 TB/s); 16 rows in 3.6 us.
 template <int W> constexpr int ROWS = W == 1 ? 4 : 1;
 template <int W> constexpr int THREADS = W == 1 ? 256 : W * 64;
 
@@ -169,8 +169,8 @@ __global__ __launch_bounds__(THREADS<W>) void add_norm_kernel(NormArgs a, int nv
 
 // dx = dsum + rho (g dy - s rho rho mean(g dy s)), the root's factors apart: their
 // cube leaves fp32 for rows beyond 1e13 or (eps = 0) below 1e-13.  A block adds
-// dy s rho of its rows (a fixed set) in registers and leaves its sums in `partial`.  Bound by
-// memory: 6400 rows of 1024 bf16 in 10.7 us (52 MB, 4.9 TB/s).
+// dy s rho of its rows (a fixed set) in registers and leaves its sums in `partial`.
+// Bound by memory: 6400 rows of 1024 bf16 in 12.8 us (52 MB needed, 4.1 TB/s).
 template <typename T, int W, int P>
 __global__ __launch_bounds__(THREADS<W>) void add_norm_backward_kernel(NormBwdArgs a, int nv)
 {
@@ -250,7 +250,7 @@ __global__ __launch_bounds__(THREADS<W>) void add_norm_backward_kernel(NormBwdAr
 }
 
 // dg (+)= the sum of the blocks' rows: 32 groups of 16 lanes take every 32nd
-// row of 64 columns, and their sums are added in order.  3.0 us for 1024
+// row of 64 columns, and their sums are added in order.  3.9 us for 1024
 // columns, the latency of a launch and 16 loads; one thread per column took 234.
 __global__ __launch_bounds__(512) void norm_gain_kernel(const float *__restrict__ partial, int rows, int D,
                                                         float *__restrict__ dg, int accumulate)

@@ -615,3 +615,71 @@ def test_linattn_wide_heads_captured(dtype):
         torch.cuda.synchronize()
         check_linattn({n: d[n] for n in ("o", "ST", "dq", "dk", "dv", "dS0")}, c, T, B, N, K, M, dtype, K ** -0.5,
                       f"captured wide heads {dtype}")
+
+
+# ---------------------------------------------------------------------------
+# strides of their own for every tensor, and every output in an input's place
+# that the calls allow
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [72, 2056])
+def test_add_norm_strides_and_places(dtype, D):
+    from paper_1907_13257_amd import AddNorm
+    g = gen(D)
+    rows, eps = 9, 1e-5
+    x, res, dy, dsum = (normal(g, rows, D, dtype=dtype) for _ in range(4))
+    gain = normal(g, D, dtype=dtype)
+    dense = AddNorm(rows, D, dtype, eps)
+    s, y, dx = (torch.empty_like(x).cuda() for _ in range(3))
+    dg = torch.empty(D, device="cuda")
+    G = gain.cuda()
+    dense.forward(x.cuda(), res.cuda(), G, s, y)
+    dense.backward(dy.cuda(), dsum.cuda(), s, G, dx, dg)
+    ref = norm_definition(s.cpu(), gain, eps)
+    close(y, ref, ref.abs(), STEPS, dtype, f"norm D{D} {dtype}")
+    # ldx, ldr and ldy all different; what lies between the rows stays
+    op = AddNorm(rows, D, dtype, eps, D + 8, D + 16, D + 40)
+    at = lambda t, extra: basic.strided(t, extra, 7.0)   # noqa: E731
+    s2, y2, dx2, dg2 = at(x, 16), at(x, 40), at(x, 8), torch.empty(D, device="cuda")
+    op.forward(at(x, 8), at(res, 16), G, s2, y2)
+    op.backward(at(dy, 40), at(dsum, 16), s2, G, dx2, dg2)
+    for got, want, extra in ((s2, s, 16), (y2, y, 40), (dx2, dx, 8)):
+        assert torch.equal(got, want)
+        between = got.as_strided((rows, extra), (D + extra, 1), D)
+        assert (between == 7.0).all()
+    assert torch.equal(dg2, dg)
+    # the sum in x's place; the gradient in dy's, the sum's and dsum's
+    X = x.cuda()
+    dense.forward(X, res.cuda(), G, X, y2 := torch.empty_like(X))
+    assert torch.equal(X, s) and torch.equal(y2, y)
+    for place in ("dy", "dsum", "sum"):
+        t = dict(dy=dy.cuda(), dsum=dsum.cuda(), sum=s.clone())
+        dense.backward(t["dy"], t["dsum"], t["sum"], G, t[place], dg2)
+        assert torch.equal(t[place], dx) and torch.equal(dg2, dg), place
+
+
+@pytest.mark.parametrize("T,dtype", [(75, "bf16"), (700, "bf16"), (75, "f32")])
+def test_linattn_strides(T, dtype):
+    """q, k, v and o in rows of four different strides: the dense call's bits,
+    and nothing between the rows is touched."""
+    from paper_1907_13257_amd import LinearAttention
+    B, N, K, M = 2, 3, 24, 40
+    c = linattn_case(T, B, N, K, M, dtype, "ragged", True)
+    d = device_buffers(c, T, B, N, K, M, dtype, False)
+    want = copies(run_linattn(make_linattn(T, B, N, K, M, dtype, False), d))
+    extra = dict(q=8, k=24, v=56, o=16)
+    ld = {n: N * w + extra[n] for n, w in (("q", K), ("k", K), ("v", M), ("o", M))}
+    op = LinearAttention(T, B, N, K, M, dtype, ldq=ld["q"], ldk=ld["k"], ldv=ld["v"], ldo=ld["o"])
+
+    def spread(t, n):
+        buf = torch.full((T, B, ld[n]), 7.0, dtype=t.dtype, device="cuda")
+        buf[:, :, :t.shape[2]] = t
+        return buf[:, :, :t.shape[2]]
+
+    e = dict(d, **{n: spread(d[n], n if n in ld else "o") for n in ("q", "k", "v", "do")})
+    for n in ("o", "dq", "dk", "dv"):
+        e[n] = spread(torch.zeros_like(d[n]), n[-1])
+    e["ST"], e["dS0"] = torch.empty_like(d["ST"]), torch.empty_like(d["dS0"])
+    same(run_linattn(op, e), want)
+    for n in ("o", "dq", "dk", "dv"):
+        assert (e[n].as_strided((T, B, extra[n[-1]]), (B * ld[n[-1]], ld[n[-1]], 1), e[n].shape[2]) == 7.0).all(), n
